@@ -308,6 +308,105 @@ int ibert_classifier_packed_i8(ibert_ctx* ctx, const int8_t* x, const int32_t* c
                                const int8_t* w, const double* S_w, const int32_t* bias, int N, int32_t* logits,
                                double* S_ret);
 
+/* ---- generation: one token after the other over a paged key-value cache --------------------------------------
+   The paper treats encoders only.  The operations below are what the same integer arithmetic needs to run a decoder:
+   positions inside the heads, a causal order, grouped heads, and a cache of the keys and values seen so far.  Head
+   size 64 throughout; `heads` query heads share kv_heads key and value heads, heads a multiple of kv_heads (query head
+   h reads key head h / (heads / kv_heads)).
+
+   The cache is a pool of pages.  k_cache and v_cache: int8 [n_pages][kv_heads][page_size][64], page_size a power of two
+   from 16 to 256; token j of sequence b lies in row j mod page_size of page block_tables[b][j / page_size]
+   (block_tables: int32 [B][max_pages]).  The `slot` of a token is page * page_size + row.  The int32 arrays of this
+   section need 4-byte alignment only.
+
+   A step is: ibert_kv_slots (places for the new tokens), ibert_linear_i8 (out_kind 3 or 0: Q | K | V), ibert_qkv_rope_i8
+   (norm, rotation, int8, into the cache), then ibert_attention_window_i8 for prompts or ibert_attention_decode_i8 for
+   single tokens. */
+
+/* Places in the cache for the new tokens of B requests, computed on the GPU.  lens[b]: tokens request b holds;
+   new_lens[b]: tokens it gets now (0 or more), or a negative number: the request has ended.  free_pages: a stack of the
+   pages nobody holds, *n_free of them, room for free_capacity.  In this order
+     - the pages of ended requests go onto the stack, in the order of requests and of their tables;
+     - pages are taken from its top for the others, in the same order, and written into block_tables behind the
+       ceil(lens[b] / page_size) entries in use;
+     - cu_seqlens [B+1] receives the running count of new tokens, and for new token i = cu_seqlens[b] + j of request b
+       positions[i] = lens[b] + j and slots[i] its slot; entries from cu_seqlens[B] to max_tokens - 1 get slot -1 and
+       position 0 (ibert_qkv_rope_i8 stores nothing for slot -1);
+     - lens_out[b] = lens[b] + new_lens[b] (0: ended) and *n_free_out are the lengths and the stack after the step.
+   lens_out may be lens and n_free_out may be n_free; no other arrays may overlap.  New tokens past max_tokens in the
+   running count are left out.  A token without a page (the stack is empty, or the request's table full) gets slot -1, its
+   page's entry -1, and does not count in lens_out.  Both record IBERT_ERR_VALUE_RANGE in the context's status, as do lengths
+   outside [0, max_pages * page_size] and an *n_free outside [0, free_capacity] (taken as the nearest bound).
+   B in [0, 8192], max_pages * page_size and B * max_pages below 2^31, max_tokens and free_capacity below 2^31. */
+int ibert_kv_slots(ibert_ctx* ctx, const int32_t* lens, const int32_t* new_lens, int32_t* block_tables, int B,
+                   int max_pages, int page_size, int32_t* free_pages, int64_t free_capacity, const int32_t* n_free,
+                   int64_t max_tokens, int32_t* lens_out, int32_t* n_free_out, int32_t* cu_seqlens, int32_t* slots,
+                   int32_t* positions);
+
+/* Host, pure.  Rotation frequencies of a head whose first rot_dim dimensions are rotated:
+   inv_freq[i] = base^(-2i / rot_dim), i < rot_dim / 2, slowed down for contexts `stretch` times as long as the trained
+   one (stretch >= 1; 1: unchanged): a pair that turns more than high_turns times within trained_len positions is kept, one
+   that turns fewer than low_turns times is divided by stretch, in between the two are blended linearly in the number of
+   turns.  trained_len = 0 divides all of them (positions scaled by 1 / stretch).
+   IBERT_ERR_SHAPE: rot_dim not a multiple of 8 in [8, 64]; IBERT_ERR_ARG: base <= 1, stretch < 1, trained_len < 0,
+   not 0 <= low_turns < high_turns, or a value that is not finite. */
+int ibert_rope_frequencies(int rot_dim, double base, double stretch, double trained_len, double low_turns,
+                           double high_turns, double* inv_freq);
+/* Host, pure.  Rows pos0 .. pos0 + n - 1 of the rotation table that ibert_qkv_rope_i8 reads from device memory:
+   rows[p][2i], rows[p][2i+1] = round-half-up(2^14 factor cos a), round-half-up(2^14 factor sin a) with the angle
+   a = (pos0 + p) inv_freq[i] in double precision.  factor in (0, 1.99] (an attention temperature; usually 1). */
+int ibert_rope_rows(const double* inv_freq, int rot_dim, int64_t pos0, int64_t n, double factor, int16_t* rows);
+
+typedef struct ibert_rope_desc {
+  int32_t heads, kv_heads;
+  int32_t in_bits;            /* 8: qkv is int8; 16: Q16 values in int16 (ibert_linear_i8, out_kind 3) */
+  int32_t rot_dim;            /* leading dimensions of a head that are rotated: 0 or a multiple of 8 up to 64 */
+  int32_t interleaved;        /* 0: pair i is (i, i + rot_dim / 2); 1: pair i is (2i, 2i + 1) */
+  int32_t page_size;          /* of the cache (ignored without one) */
+  int64_t n_pages;
+  int64_t max_pos;            /* rows of the rotation table */
+  const int16_t* rope;        /* device [max_pos][rot_dim], 16-byte aligned; ignored for rot_dim 0 */
+  const double *gamma_q, *gamma_k;   /* host [64] each: norm of every query / key head; both NULL: no norm */
+  double S_in, S_q, S_k, S_v; /* scale of qkv; scales of the int8 results */
+} ibert_rope_desc;
+
+/* Q | K | V of T new tokens made ready for attention: every query and key head is normed (x / rms(x) * gamma), rotated by
+   its token's position and requantized to int8 at S_q / S_k; value heads are requantized to S_v.  With integers
+     ss = sum x^2,  r = max(ISqrt(ss 2^s0), 1), s0 = 16 (int8) or 10 (int16),  l = bit length of r,
+     rho = floor(2^(l+29) / r),  b_i = round-half-up(|gamma_i| (128 / S) 2^g) with the sign of gamma_i, g the largest integer
+     up to 16 that keeps every |gamma_i| (128 / S) 2^g <= 32767,
+     u_i = clamp((x_i b_i rho + 2^(sh-1)) >> sh, +-32767), sh = l + 26 - s0/2 + g      (scale S / 128)
+   (no norm: u_i = requant(x_i; dyadic(128 S_in / S), 32767)), rotated pairs y_a = u_a c - u_b s, y_b = u_a s + u_b c with
+   (c, s) from the table, other dimensions y = 2^14 u, and the result clamp((y + 2^20) >> 21, +-127).
+   qkv: device [T][(heads + 2 kv_heads) 64], columns Q | K | V.  positions: device int32 [T] (may be NULL if rot_dim is 0).
+   out: device int8, with_kv 1: [T][(heads + 2 kv_heads) 64], the layout of qkv; with_kv 0: [T][heads 64], Q alone.
+   k_cache, v_cache, slots (device int32 [T]): K and V also go to their slots of the cache; slot -1 stores nothing; all three
+   NULL: no cache.  Two tokens must not have the same slot.  out and the cache must not overlap qkv or each other.
+   S_ret (host, may be NULL) receives S_q, S_k, S_v.
+   A position outside [0, max_pos) (taken as 0) or a slot outside [-1, n_pages * page_size) (taken as -1) records
+   IBERT_ERR_VALUE_RANGE in the context's status.  n_pages * page_size below 2^31; table entries with c^2 + s^2 <= 2^30. */
+int ibert_qkv_rope_i8(ibert_ctx* ctx, const ibert_rope_desc* desc, const void* qkv, int64_t T, const int32_t* positions,
+                      int with_kv, int8_t* out, const int32_t* slots, int8_t* k_cache, int8_t* v_cache, double* S_ret);
+
+/* Attention of ONE new token per sequence over the paged cache, which already holds the token's own key and value:
+   q int8 [B][heads 64] at S_q, out int8 [B][heads 64] at S_ctx (*S_ret).  lens: device int32 [B], tokens in the cache
+   (the new one included), at most max_len; a sequence of length 0 yields 0.  Key j is visible if j < lens[b] and
+   (window = 0, or j >= lens[b] - window, or j < sinks): a sliding window, and first tokens that stay visible.  Pages
+   that hold no visible key are not looked at.  With e_j the i-exp (Algorithm 3) of the distance of s_j = q k_j (scale
+   S_q S_k / 8) from the maximum of the visible keys and b_w = floor(p_max 2^24 / i-exp(0)):
+     w_j = (e_j b_w + 2^23) >> 24 in [0, p_max],  O = sum w_j v_j,  W = sum w_j,  l = bit length of W,
+     R = floor(b 2^(l-1) / W) with (b, c) = dyadic(S_v / S_ctx),  out = clamp((O R + 2^(c+l-2)) >> (c+l-1), +-127)
+   -- weights relative to the row's maximum, divided by their sum at the end.  (ibert_attention_i8 divides first; over
+   thousands of keys all of its u8 probabilities would be 0.)
+   At most 65536 visible keys: min(max_len, window + sinks if window > 0) <= 65536, else IBERT_ERR_SHAPE; window, sinks >= 0;
+   max_len <= max_pages * page_size.  A length above max_len (taken as max_len) or below 0, and a visible key on a page
+   outside [0, n_pages) (the key is left out), record IBERT_ERR_VALUE_RANGE in the context's status.
+   IBERT_ERR_SCALE_RANGE also for score scales so coarse that floor(ln2 / (S_q S_k / 8)) <= 2; p_max in {255, 127}. */
+int ibert_attention_decode_i8(ibert_ctx* ctx, const int8_t* q, const int8_t* k_cache, const int8_t* v_cache,
+                              const int32_t* block_tables, const int32_t* lens, int B, int max_len, int max_pages,
+                              int64_t n_pages, int page_size, int heads, int kv_heads, int window, int sinks, double S_q,
+                              double S_k, double S_v, double S_ctx, int p_max, int8_t* out, double* S_ret);
+
 /* ---- h-GELU, the comparison function of the paper (Eq. 6; Table 1, Table 3) --------------------
    h-GELU(x) = x ReLU6(1.702 x + 3) / 6.  The paper notes that it can be computed with integers
    but gives no integer algorithm; this library's reading keeps it parallel to i-GELU: the same
@@ -353,7 +452,9 @@ int ibert_encoder_graph_destroy(ibert_graph* graph);
 /* Per-kernel device timing (CUDA events recorded on the context's stream around every launch
    between begin and end).  No counterpart in the paper: measurement support only.
    ibert_profile_end synchronizes the stream and fills, per kernel class below, the summed
-   device milliseconds and the number of launches (arrays of IBERT_NUM_KERNEL_CLASSES). */
+   device milliseconds and the number of launches (arrays of IBERT_NUM_KERNEL_CLASSES).  The calls
+   for generation count as ATTENTION (both attentions) and LAYERNORM (ibert_qkv_rope_i8); ibert_kv_slots
+   is not counted. */
 enum {
   IBERT_K_GEMM_QKV = 0,      /* ibert_linear_i8 kind 0 / layer step QKV   */
   IBERT_K_ATTENTION = 1,

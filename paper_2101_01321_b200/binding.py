@@ -39,6 +39,12 @@ class LayerDesc(C.Structure):
             "gamma1", "beta1", "gamma2", "beta2")] + [(n, C.c_double) for n in SCALE_NAMES]
 
 
+class RopeDesc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("heads", "kv_heads", "in_bits", "rot_dim", "interleaved", "page_size")] + [
+        ("n_pages", C.c_int64), ("max_pos", C.c_int64), ("rope", C.c_void_p), ("gamma_q", C.c_void_p), ("gamma_k", C.c_void_p)] + [
+        (n, C.c_double) for n in ("S_in", "S_q", "S_k", "S_v")]
+
+
 def lib():
     """Loads the C-ABI library; fails loudly if it has not been built."""
     global _lib
@@ -103,6 +109,14 @@ def lib():
         L.ibert_profile_end.argtypes = [vp, vp, vp]
         L.ibert_profile_begin.restype = i32
         L.ibert_profile_end.restype = i32
+        L.ibert_kv_slots.argtypes = [vp, vp, vp, vp, i32, i32, i32, vp, i64, vp, i64, vp, vp, vp, vp, vp]
+        L.ibert_rope_frequencies.argtypes = [i32, dbl, dbl, dbl, dbl, dbl, vp]
+        L.ibert_rope_rows.argtypes = [vp, i32, i64, i64, dbl, vp]
+        L.ibert_qkv_rope_i8.argtypes = [vp, C.POINTER(RopeDesc), vp, i64, vp, i32, vp, vp, vp, vp, vp]
+        L.ibert_attention_decode_i8.argtypes = [vp, vp, vp, vp, vp, vp, i32, i32, i32, i64, i32, i32, i32, i32, i32, dbl, dbl, dbl,
+                                                dbl, i32, vp, vp]
+        for name in ("ibert_kv_slots", "ibert_rope_frequencies", "ibert_rope_rows", "ibert_qkv_rope_i8", "ibert_attention_decode_i8"):
+            getattr(L, name).restype = i32
         for name in ("ibert_create", "ibert_destroy", "ibert_last_status", "ibert_dyadic_from_double",
                      "ibert_linear_i8", "ibert_linear_gelu_i8", "ibert_linear_layernorm_i8", "ibert_softmax_i", "ibert_gelu_i",
                      "ibert_layernorm_i", "ibert_attention_i8", "ibert_layer_create", "ibert_layer_destroy",
@@ -158,6 +172,23 @@ def ibert_layernorm_i_static_status(stream: torch.cuda.Stream | None = None) -> 
     """Synchronizes `stream` and returns (then clears) the device-side status of the
     allocation-free LayerNorm calls on the current device."""
     return int(lib().ibert_layernorm_i_static_status(None if stream is None else stream.cuda_stream))
+
+
+def ibert_rope_frequencies(rot_dim: int, base: float = 10000.0, stretch: float = 1.0, trained_len: float = 0.0,
+                           low_turns: float = 1.0, high_turns: float = 32.0) -> np.ndarray:
+    """Rotation frequencies, slowed down for contexts ``stretch`` times as long as the trained one."""
+    f = np.zeros(max(rot_dim // 2, 1), dtype=np.float64)
+    _chk(lib().ibert_rope_frequencies(rot_dim, base, stretch, trained_len, low_turns, high_turns, f.ctypes.data),
+         "ibert_rope_frequencies")
+    return f
+
+
+def ibert_rope_rows(inv_freq, n: int, factor: float = 1.0, pos0: int = 0) -> np.ndarray:
+    """Rows of the rotation table for positions pos0 .. pos0 + n - 1: int16 [n, 2 * len(inv_freq)]."""
+    f = _host(inv_freq, np.float64)
+    rows = np.zeros((n, 2 * f.size), dtype=np.int16)
+    _chk(lib().ibert_rope_rows(f.ctypes.data, 2 * f.size, pos0, n, factor, rows.ctypes.data), "ibert_rope_rows")
+    return rows
 
 
 class Context:
@@ -453,6 +484,86 @@ class Context:
                                               _dev(w, torch.int8), sw.ctypes.data, _dev(bias, torch.int32), N,
                                               _dev(out, torch.int32), S_ret.ctypes.data), "ibert_classifier_packed_i8")
         return out, S_ret
+
+    # ------------------------------------------------------------------ generation over a paged cache
+    def ibert_kv_slots(self, lens: torch.Tensor, new_lens: torch.Tensor, block_tables: torch.Tensor, free_pages: torch.Tensor,
+                       n_free: torch.Tensor, page_size: int, max_tokens: int | None = None, lens_out: torch.Tensor | None = None,
+                       n_free_out: torch.Tensor | None = None, cu_seqlens: torch.Tensor | None = None,
+                       slots: torch.Tensor | None = None, positions: torch.Tensor | None = None):
+        """Pages, block tables, slots and positions of a step's new tokens (``new_lens`` negative: the request has ended);
+        all device int32.  Returns (lens_out, n_free_out, cu_seqlens, slots, positions); ``block_tables`` and ``free_pages``
+        are updated in place.  ``slots`` / ``positions`` or ``max_tokens`` give the room for new tokens."""
+        B = lens.numel()
+        assert new_lens.numel() == B and block_tables.shape[0] == B and n_free.numel() == 1
+        if slots is None:
+            slots = lens.new_empty(max_tokens)
+        if positions is None:
+            positions = slots.new_empty(slots.numel())
+        assert positions.numel() == slots.numel() and max_tokens in (None, slots.numel())
+        lens_out = torch.empty_like(lens) if lens_out is None else lens_out
+        n_free_out = torch.empty_like(n_free) if n_free_out is None else n_free_out
+        cu_seqlens = lens.new_empty(B + 1) if cu_seqlens is None else cu_seqlens
+        assert lens_out.numel() == B and n_free_out.numel() == 1 and cu_seqlens.numel() == B + 1
+        i32 = torch.int32
+        _chk(lib().ibert_kv_slots(self.h, _dev(lens, i32), _dev(new_lens, i32), _dev(block_tables, i32), B, block_tables.shape[1],
+                                  page_size, _dev(free_pages, i32), free_pages.numel(), _dev(n_free, i32), slots.numel(),
+                                  _dev(lens_out, i32), _dev(n_free_out, i32), _dev(cu_seqlens, i32), _dev(slots, i32),
+                                  _dev(positions, i32)), "ibert_kv_slots")
+        return lens_out, n_free_out, cu_seqlens, slots, positions
+
+    def ibert_qkv_rope_i8(self, qkv: torch.Tensor, S_in: float, heads: int, kv_heads: int, S_q: float, S_k: float, S_v: float,
+                          gamma_q=None, gamma_k=None, rope: torch.Tensor | None = None, positions: torch.Tensor | None = None,
+                          interleaved: bool = False, slots: torch.Tensor | None = None, k_cache: torch.Tensor | None = None,
+                          v_cache: torch.Tensor | None = None, with_kv: bool = True, out: torch.Tensor | None = None):
+        """Norm of the query and key heads, rotary positions and int8 in one pass; ``qkv`` int8 or int16 [T, (heads +
+        2 kv_heads) * 64], ``rope`` device int16 [positions, rot_dim] (``ibert_rope_rows``), caches int8 [pages, kv_heads,
+        page_size, 64].  Returns (out, (S_q, S_k, S_v))."""
+        n = (heads + 2 * kv_heads) * 64
+        T = qkv.numel() // n
+        assert qkv.numel() == T * n and qkv.dtype in (torch.int8, torch.int16)
+        d = RopeDesc(heads, kv_heads, 8 * qkv.element_size(), 0, int(interleaved), 0, 0, 0, None, None, None, S_in, S_q, S_k, S_v)
+        if gamma_q is not None:
+            gq = _host(gamma_q, np.float64)
+            assert gq.size == 64
+            d.gamma_q = gq.ctypes.data
+        if gamma_k is not None:
+            gk = _host(gamma_k, np.float64)
+            assert gk.size == 64
+            d.gamma_k = gk.ctypes.data
+        if rope is not None:
+            d.max_pos, d.rot_dim = rope.shape
+            d.rope = _dev(rope, torch.int16)
+            assert positions is not None and positions.numel() == T
+        if k_cache is not None:
+            assert k_cache.dim() == 4 and k_cache.shape[1] == kv_heads and k_cache.shape[3] == 64
+            assert v_cache is not None and v_cache.shape == k_cache.shape and slots is not None and slots.numel() == T
+            d.n_pages, _, d.page_size, _ = k_cache.shape
+        if out is None:
+            out = torch.empty((T, n if with_kv else heads * 64), dtype=torch.int8, device=qkv.device)
+        assert out.numel() == T * (n if with_kv else heads * 64)
+        S_ret = (C.c_double * 3)()
+        _chk(lib().ibert_qkv_rope_i8(self.h, C.byref(d), _dev(qkv, qkv.dtype), T, _dev(positions, torch.int32), int(with_kv),
+                                     _dev(out, torch.int8), _dev(slots, torch.int32), _dev(k_cache, torch.int8),
+                                     _dev(v_cache, torch.int8), S_ret), "ibert_qkv_rope_i8")
+        return out, tuple(S_ret)
+
+    def ibert_attention_decode_i8(self, q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, block_tables: torch.Tensor,
+                                  lens: torch.Tensor, max_len: int, heads: int, S_q: float, S_k: float, S_v: float, S_ctx: float,
+                                  window: int = 0, sinks: int = 0, p_max: int = 255, out: torch.Tensor | None = None):
+        """Attention of one new token per sequence over the paged cache; ``q`` int8 [B, heads * 64], ``lens`` device int32 [B]
+        (the new token included), caches int8 [pages, kv_heads, page_size, 64]."""
+        B, max_pages = block_tables.shape
+        n_pages, kv_heads, page_size, D = k_cache.shape
+        assert D == 64 and v_cache.shape == k_cache.shape and q.numel() == B * heads * 64 and lens.numel() == B
+        if out is None:
+            out = q.new_empty((B, heads * 64))
+        assert out.numel() == q.numel()
+        S_ret = C.c_double()
+        _chk(lib().ibert_attention_decode_i8(self.h, _dev(q, torch.int8), _dev(k_cache, torch.int8), _dev(v_cache, torch.int8),
+                                             _dev(block_tables, torch.int32), _dev(lens, torch.int32), B, max_len, max_pages, n_pages,
+                                             page_size, heads, kv_heads, window, sinks, S_q, S_k, S_v, S_ctx, p_max,
+                                             _dev(out, torch.int8), C.byref(S_ret)), "ibert_attention_decode_i8")
+        return out, S_ret.value
 
     # ------------------------------------------------------------------ encoder layer
     def ibert_layer_create(self, params: dict) -> "Layer":

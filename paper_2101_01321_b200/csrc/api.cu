@@ -1,5 +1,6 @@
 // C-ABI entry points of libibert_b200: argument validation, constant derivation,
 // launch.  No entry point synchronizes (except ibert_last_status) and none has a CPU path.
+#include <algorithm>
 #include <cmath>
 #include <cstdlib>
 #include <cstring>
@@ -1076,6 +1077,162 @@ int ibert_encoder_graph_destroy(ibert_graph* g) {
   cudaStreamSynchronize(g->ctx->stream);
   graph_free(g);
   return IBERT_OK;
+  });
+}
+
+// ---------------------------------------------------------------------- generation over a paged cache
+
+static bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+static int log2_page(int page_size) {              // -1: not a power of two from 16 to 256
+  for (int l = 4; l <= 8; ++l)
+    if (page_size == 1 << l) return l;
+  return -1;
+}
+
+int ibert_kv_slots(ibert_ctx* ctx, const int32_t* lens, const int32_t* new_lens, int32_t* block_tables, int B,
+                   int max_pages, int page_size, int32_t* free_pages, int64_t free_capacity, const int32_t* n_free,
+                   int64_t max_tokens, int32_t* lens_out, int32_t* n_free_out, int32_t* cu_seqlens, int32_t* slots,
+                   int32_t* positions) {
+  return guarded([&]() -> int {
+  if (!ctx || B < 0 || max_tokens < 0 || free_capacity < 0 || max_pages < 0) return IBERT_ERR_ARG;
+  const int log_page = log2_page(page_size);
+  const int64_t limit = int64_t(1) << 31;
+  if (log_page < 0 || B > kMaxRequests || ((int64_t)max_pages << log_page) >= limit || (int64_t)B * max_pages >= limit ||
+      max_tokens >= limit || free_capacity >= limit)
+    return IBERT_ERR_SHAPE;
+  if (!n_free || !n_free_out || !cu_seqlens || (free_capacity > 0 && !free_pages) || (max_tokens > 0 && (!slots || !positions)) ||
+      (B > 0 && (!lens || !new_lens || !lens_out || (max_pages > 0 && !block_tables))))
+    return IBERT_ERR_ARG;
+  for (const void* p : {(const void*)lens, (const void*)new_lens, (const void*)block_tables, (const void*)free_pages,
+                        (const void*)n_free, (const void*)lens_out, (const void*)n_free_out, (const void*)cu_seqlens,
+                        (const void*)slots, (const void*)positions})
+    if (!aligned4(p)) return IBERT_ERR_ALIGN;
+  DeviceGuard guard(ctx->device);
+  return launch_kv_slots(ctx, lens, new_lens, block_tables, free_pages, n_free, B, log_page, max_pages, free_capacity,
+                         max_tokens, lens_out, n_free_out, cu_seqlens, slots, positions);
+  });
+}
+
+int ibert_rope_frequencies(int rot_dim, double base, double stretch, double trained_len, double low_turns,
+                           double high_turns, double* inv_freq) {
+  return guarded([&]() -> int {
+  if (rot_dim < 8 || rot_dim > 64 || rot_dim % 8 != 0) return IBERT_ERR_SHAPE;
+  if (!inv_freq || !std::isfinite(base) || !(base > 1.0) || !std::isfinite(stretch) || !(stretch >= 1.0) ||
+      !std::isfinite(trained_len) || !(trained_len >= 0.0))
+    return IBERT_ERR_ARG;
+  if (trained_len > 0.0 && (!std::isfinite(low_turns) || !std::isfinite(high_turns) || !(low_turns >= 0.0) || !(high_turns > low_turns)))
+    return IBERT_ERR_ARG;
+  for (int i = 0; i < rot_dim / 2; ++i) {
+    const double f = std::pow(base, -2.0 * i / rot_dim);
+    double keep = 0.0;                             // 1: as trained, 0: divided by stretch
+    if (trained_len > 0.0) {
+      const double turns = trained_len * f / 6.283185307179586;
+      keep = std::fmin(1.0, std::fmax(0.0, (turns - low_turns) / (high_turns - low_turns)));
+    }
+    inv_freq[i] = f * (keep + (1.0 - keep) / stretch);
+  }
+  return IBERT_OK;
+  });
+}
+
+int ibert_rope_rows(const double* inv_freq, int rot_dim, int64_t pos0, int64_t n, double factor, int16_t* rows) {
+  return guarded([&]() -> int {
+  if (rot_dim < 8 || rot_dim > 64 || rot_dim % 8 != 0) return IBERT_ERR_SHAPE;
+  if (!inv_freq || n < 0 || pos0 < 0 || (n > 0 && !rows)) return IBERT_ERR_ARG;
+  if (!std::isfinite(factor) || !(factor > 0.0) || factor > 1.99) return IBERT_ERR_ARG;
+  for (int i = 0; i < rot_dim / 2; ++i)
+    if (!std::isfinite(inv_freq[i])) return IBERT_ERR_ARG;
+  for (int64_t p = 0; p < n; ++p)
+    for (int i = 0; i < rot_dim / 2; ++i) {
+      const double angle = (double)(pos0 + p) * inv_freq[i];
+      rows[p * rot_dim + 2 * i] = (int16_t)std::floor(std::cos(angle) * factor * 16384.0 + 0.5);
+      rows[p * rot_dim + 2 * i + 1] = (int16_t)std::floor(std::sin(angle) * factor * 16384.0 + 0.5);
+    }
+  return IBERT_OK;
+  });
+}
+
+int ibert_qkv_rope_i8(ibert_ctx* ctx, const ibert_rope_desc* d, const void* qkv, int64_t T, const int32_t* positions,
+                      int with_kv, int8_t* out, const int32_t* slots, int8_t* k_cache, int8_t* v_cache, double* S_ret) {
+  return guarded([&]() -> int {
+  if (!ctx || !d || T < 0 || (with_kv != 0 && with_kv != 1) || (d->interleaved != 0 && d->interleaved != 1)) return IBERT_ERR_ARG;
+  if (d->heads < 1 || d->kv_heads < 1 || d->heads % d->kv_heads != 0 || d->heads > 4096 || (d->in_bits != 8 && d->in_bits != 16) ||
+      d->rot_dim < 0 || d->rot_dim > 64 || d->rot_dim % 8 != 0 || T >= (int64_t(1) << 31))
+    return IBERT_ERR_SHAPE;
+  if (!d->gamma_q != !d->gamma_k) return IBERT_ERR_ARG;
+  if (!k_cache != !v_cache || !k_cache != !slots) return IBERT_ERR_ARG;
+  RopeArgs a{};
+  if (k_cache) {
+    a.log_page = log2_page(d->page_size);
+    if (a.log_page < 0 || d->n_pages < 0 || d->n_pages >= (int64_t(1) << 31) >> a.log_page) return IBERT_ERR_SHAPE;
+    a.n_slots = d->n_pages << a.log_page;
+  }
+  if (d->rot_dim > 0 && (d->max_pos < 1 || !d->rope || (T > 0 && !positions))) return IBERT_ERR_ARG;
+  if (T > 0 && (!qkv || !out)) return IBERT_ERR_ARG;
+  if (!aligned16(qkv) || !aligned16(out) || !aligned16(k_cache) || !aligned16(v_cache) || !aligned4(slots) ||
+      (d->rot_dim > 0 && (!aligned16(d->rope) || !aligned4(positions))))
+    return IBERT_ERR_ALIGN;
+  if (!good_scale(d->S_in) || !good_scale(d->S_q) || !good_scale(d->S_k) || !good_scale(d->S_v)) return IBERT_ERR_SCALE_RANGE;
+  int rc = IBERT_OK;
+  const bool norm = d->gamma_q != nullptr;
+  if (norm) {
+    if ((rc = make_head_norm(d->gamma_q, d->S_q, a.gamma[0], &a.g[0])) || (rc = make_head_norm(d->gamma_k, d->S_k, a.gamma[1], &a.g[1])))
+      return rc;
+  } else if ((rc = dyadic((128.0 * d->S_in) / d->S_q, &a.b[0], &a.c[0])) || (rc = dyadic((128.0 * d->S_in) / d->S_k, &a.b[1], &a.c[1]))) {
+    return rc;
+  }
+  if ((rc = dyadic(d->S_in / d->S_v, &a.b[2], &a.c[2]))) return rc;
+  if (S_ret) { S_ret[0] = d->S_q; S_ret[1] = d->S_k; S_ret[2] = d->S_v; }
+  if (T == 0) return IBERT_OK;
+  a.x = qkv; a.rope = d->rope; a.positions = positions; a.slots = slots; a.k_cache = k_cache; a.v_cache = v_cache; a.out = out;
+  a.T = T; a.max_pos = d->max_pos; a.heads = d->heads; a.kv_heads = d->kv_heads; a.rot = d->rot_dim;
+  a.interleaved = d->interleaved; a.with_kv = with_kv;
+  DeviceGuard guard(ctx->device);
+  ProfileScope ps(ctx, IBERT_K_LAYERNORM);
+  return launch_qkv_rope(ctx, a, d->in_bits == 16, norm);
+  });
+}
+
+static int make_long_attn_consts(double S_q, double S_k, double S_v, double S_ctx, int p_max, LongAttnConsts* k) {
+  if (!good_scale(S_q) || !good_scale(S_k) || !good_scale(S_v) || !good_scale(S_ctx)) return IBERT_ERR_SCALE_RANGE;
+  int rc = make_exp_consts((S_q * S_k) / 8.0, p_max, &k->e);
+  if (rc) return rc;
+  if (k->e.q_ln2 <= 2 || k->e.wide_post < 0) return IBERT_ERR_SCALE_RANGE;    // the unclamped quotient is not available
+  const uint32_t top = (uint32_t)((int64_t)k->e.q_b * k->e.q_b + k->e.q_c) >> k->e.s_out;
+  k->b_w = ((uint32_t)p_max << 24) / top;
+  return dyadic(S_v / S_ctx, &k->b, &k->c);
+}
+
+static int check_long_attention(int64_t max_len, int heads, int kv_heads, int window, int sinks) {
+  if (window < 0 || sinks < 0) return IBERT_ERR_ARG;
+  if (heads < 1 || kv_heads < 1 || heads % kv_heads != 0 || heads > 4096 || max_len < 1) return IBERT_ERR_SHAPE;
+  if ((window > 0 ? std::min<int64_t>(max_len, (int64_t)window + sinks) : max_len) > kMaxVisible) return IBERT_ERR_SHAPE;
+  return IBERT_OK;
+}
+
+int ibert_attention_decode_i8(ibert_ctx* ctx, const int8_t* q, const int8_t* k_cache, const int8_t* v_cache,
+                              const int32_t* block_tables, const int32_t* lens, int B, int max_len, int max_pages,
+                              int64_t n_pages, int page_size, int heads, int kv_heads, int window, int sinks, double S_q,
+                              double S_k, double S_v, double S_ctx, int p_max, int8_t* out, double* S_ret) {
+  return guarded([&]() -> int {
+  if (!ctx || B < 0) return IBERT_ERR_ARG;
+  int rc = check_long_attention(max_len, heads, kv_heads, window, sinks);
+  if (rc) return rc;
+  const int log_page = log2_page(page_size);
+  if (log_page < 0 || max_pages < 0 || max_len > (int64_t)max_pages << log_page || n_pages < 0 ||
+      n_pages >= (int64_t(1) << 31) >> log_page || (int64_t)B * heads >= (int64_t(1) << 24))
+    return IBERT_ERR_SHAPE;
+  if (B > 0 && (!q || !k_cache || !v_cache || !block_tables || !lens || !out)) return IBERT_ERR_ARG;
+  if (!aligned16(q) || !aligned16(k_cache) || !aligned16(v_cache) || !aligned16(out) || !aligned4(block_tables) || !aligned4(lens))
+    return IBERT_ERR_ALIGN;
+  LongAttnConsts k{};
+  if ((rc = make_long_attn_consts(S_q, S_k, S_v, S_ctx, p_max, &k))) return rc;
+  if (S_ret) *S_ret = S_ctx;
+  if (B == 0) return IBERT_OK;
+  DeviceGuard guard(ctx->device);
+  ProfileScope ps(ctx, IBERT_K_ATTENTION);
+  return launch_attention_decode(ctx, q, k_cache, v_cache, block_tables, lens, B, max_pages, (int)n_pages, log_page, max_len,
+                                 heads, kv_heads, window, sinks, k, out);
   });
 }
 

@@ -327,6 +327,22 @@ __device__ __forceinline__ RowDivisor make_row_divisor(uint32_t sum, uint32_t p_
 __device__ __forceinline__ uint32_t softmax_quotient(uint32_t e, const RowDivisor& r) {
   return __umulhi(e << r.pre, r.m) >> r.post;
 }
+// The mean of values weighted by w (LongAttnConsts): R = floor(b 2^(l-1) / W) with l the bit length of the sum W of the
+// weights is b / W in units of 2^-(l-1) and fits 31 bits; out = clamp((O R + 2^(sh-1)) >> sh, +-127), sh = c + l - 1.
+// (W is at least p_max where a key is visible, else 0: the result is 0.)
+struct RowShare {
+  int32_t r;
+  int sh;
+};
+__device__ __forceinline__ RowShare row_share(uint32_t W, const LongAttnConsts& k) {
+  if (W == 0) return {0, 1};
+  const int l = 32 - __clz(W);
+  return {(int32_t)(((uint64_t)(uint32_t)k.b << (l - 1)) / W), k.c + l - 1};
+}
+__device__ __forceinline__ int32_t weighted_mean(int32_t o, const RowShare& s) {
+  return requant_add(o, s.r, int64_t(1) << (s.sh - 1), s.sh, 127);
+}
+
 // the common case pre == 0 (row sum >= 2^8)
 __device__ __forceinline__ uint32_t softmax_quotient_nopre(uint32_t e, const RowDivisor& r) {
   return __umulhi(e, r.m) >> r.post;

@@ -158,6 +158,26 @@ int make_exp_consts(double S, int p_max, ExpConsts* k) {
   return IBERT_OK;
 }
 
+// Multipliers of the per-head norm: gamma 128 / S_out in units of 2^-g, 16 bits, g common to the head (at most 16; below -8
+// the shift of the kernel would leave its range).
+int make_head_norm(const double* gamma, double S_out, int16_t* b, int32_t* g) {
+  const double unit = 128.0 / S_out;
+  double top = 0.0;
+  for (int i = 0; i < 64; ++i) {
+    if (!std::isfinite(gamma[i] * unit)) return IBERT_ERR_SCALE_RANGE;
+    top = std::max(top, std::fabs(gamma[i] * unit));
+  }
+  int e = top > 0.0 ? (int)std::min(16.0, std::floor(std::log2(32767.0 / top))) : 16;
+  while (std::floor(std::ldexp(top, e) + 0.5) > 32767.0) --e;     // (a logarithm rounded up)
+  if (e < -8) return IBERT_ERR_SCALE_RANGE;
+  for (int i = 0; i < 64; ++i) {
+    const double m = std::floor(std::ldexp(std::fabs(gamma[i] * unit), e) + 0.5);
+    b[i] = (int16_t)(gamma[i] < 0.0 ? -m : m);
+  }
+  *g = e;
+  return IBERT_OK;
+}
+
 // Exactness is needed up to (bl - s_out) q here, by the argument above; every q <= 16787 has it, and below q = 16 it
 // reaches to 31 q.  (q = 1: floor((d' + 1) (2^32 - 1) / 2^32) = d'.)
 int make_row_exp_consts(double S, int p_max, RowExpConsts* k) {

@@ -297,6 +297,43 @@ struct AttnConsts {
   int32_t b2, fast;        // upper-word form: (v * b2 + 2^31) >> 32 with b2 = b << (32 - c)
 };
 
+// Attention over long sequences (windowed and paged): weights relative to the row's maximum, divided by their sum at
+// the end.  w = (e b_w + 2^23) >> 24 in [0, p_max] with b_w = floor(p_max 2^24 / i-exp(0)); the result is the weighted
+// mean of the values at dyadic(S_v / S_ctx) = b / 2^c.
+struct LongAttnConsts {
+  ExpConsts e;
+  uint32_t b_w;
+  int32_t b, c;
+};
+constexpr int kMaxVisible = 65536;       // visible keys per query: 255 * 128 * 65536 < 2^31
+
+int launch_attention_decode(ibert_ctx* ctx, const int8_t* q, const int8_t* k_cache, const int8_t* v_cache,
+                            const int32_t* tables, const int32_t* lens, int B, int max_pages, int n_pages, int log_page,
+                            int max_len, int heads, int kv_heads, int window, int sinks, const LongAttnConsts& k,
+                            int8_t* out);
+
+constexpr int kMaxRequests = 8192;       // of one launch_kv_slots
+int launch_kv_slots(ibert_ctx* ctx, const int32_t* lens, const int32_t* new_lens, int32_t* tables, int32_t* stack,
+                    const int32_t* n_free, int B, int log_page, int max_pages, int64_t capacity, int64_t max_tokens,
+                    int32_t* lens_out, int32_t* n_free_out, int32_t* cu, int32_t* slots, int32_t* positions);
+
+struct RopeArgs {
+  const void* x;                         // [T][(heads + 2 kv_heads) 64] int8 or int16
+  const int16_t* rope;                   // [max_pos][rot]: (cos, sin) of every pair in units of 2^-14
+  const int32_t *positions, *slots;      // [T]
+  int8_t *k_cache, *v_cache;             // [pages][kv_heads][page][64], or null
+  int8_t* out;                           // [T][heads 64], with_kv: [T][(heads + 2 kv_heads) 64]
+  int32_t* status;
+  int64_t T, max_pos, n_slots;
+  int32_t heads, kv_heads, rot, interleaved, with_kv, log_page;
+  int32_t per;                           // heads that eight lanes take one after the other
+  int32_t b[3], c[3];                    // Q, K without a norm: dyadic(128 S_in / S_out); V: dyadic(S_in / S_v)
+  int32_t g[2];                          // with a norm: gamma 128 / S_out in units of 2^-g, 16 bits
+  int16_t gamma[2][64];
+};
+int make_head_norm(const double* gamma, double S_out, int16_t* b, int32_t* g);
+int launch_qkv_rope(ibert_ctx* ctx, RopeArgs a, bool x_is_i16, bool norm);
+
 // GEMM + residual + i-LayerNorm in one kernel (cluster of H / 256 CTAs per 128-token tile):
 // out = LN(requant_Q16(x w^T + bias) + rescale(res)).  `gemm_ln_supported` tells whether the
 // shapes and constants allow it; otherwise run launch_gemm_i8 (Q16) followed by launch_layernorm.

@@ -335,6 +335,15 @@ __device__ __forceinline__ void red_add_cluster_s32(uint32_t cluster_addr, int32
 __device__ __forceinline__ void red_add_cluster_u64(uint32_t cluster_addr, uint64_t v) {
   asm volatile("red.relaxed.cluster.shared::cluster.add.u64 [%0], %1;" ::"r"(cluster_addr), "l"(v) : "memory");
 }
+// plain stores into and loads from another CTA's shared memory (ordered by a cluster barrier)
+__device__ __forceinline__ void st_cluster_s32(uint32_t cluster_addr, int32_t v) {
+  asm volatile("st.shared::cluster.s32 [%0], %1;" ::"r"(cluster_addr), "r"(v) : "memory");
+}
+__device__ __forceinline__ int32_t ld_cluster_s32(uint32_t cluster_addr) {
+  int32_t v;
+  asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(cluster_addr) : "memory");
+  return v;
+}
 __device__ __forceinline__ void fence_acq_rel_cluster() { asm volatile("fence.acq_rel.cluster;" ::: "memory"); }
 // arrive that releases this thread's (and, after a fence, its CTA's) earlier writes to the whole cluster
 __device__ __forceinline__ void mbar_arrive_remote_release(uint32_t cluster_addr) {
