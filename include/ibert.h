@@ -388,6 +388,19 @@ typedef struct ibert_rope_desc {
 int ibert_qkv_rope_i8(ibert_ctx* ctx, const ibert_rope_desc* desc, const void* qkv, int64_t T, const int32_t* positions,
                       int with_kv, int8_t* out, const int32_t* slots, int8_t* k_cache, int8_t* v_cache, double* S_ret);
 
+/* Causal attention of packed prompts: qkv int8 [total_tokens][(heads + 2 kv_heads) 64], columns Q | K | V (what
+   ibert_qkv_rope_i8 writes with with_kv = 1), sequence b in rows cu_seqlens[b] .. cu_seqlens[b+1] - 1 (device int32 [B+1],
+   non-decreasing from 0, every length at most max_len); out int8 [total_tokens][heads 64] at S_ctx (*S_ret).  A query sees the
+   keys of its own sequence up to its own position; with window > 0 only the last `window` of them (itself included) and the
+   first `sinks` of the sequence.  Rows from cu_seqlens[B] on are left as they were.  Weights and result as defined for
+   ibert_attention_decode_i8 below -- a token's context is the same bit for bit whichever of the two computes it.
+   At most 65536 visible keys: min(max_len, window + sinks if window > 0) <= 65536, else IBERT_ERR_SHAPE.  A sequence longer
+   than max_len records IBERT_ERR_VALUE_RANGE in the context's status; its queries then see at most their last max_len keys.
+   total_tokens < 2^31 - 256; scale and p_max errors as below. */
+int ibert_attention_window_i8(ibert_ctx* ctx, const int8_t* qkv, const int32_t* cu_seqlens, int B, int max_len,
+                              int64_t total_tokens, int heads, int kv_heads, int window, int sinks, double S_q, double S_k,
+                              double S_v, double S_ctx, int p_max, int8_t* out, double* S_ret);
+
 /* Attention of ONE new token per sequence over the paged cache, which already holds the token's own key and value:
    q int8 [B][heads 64] at S_q, out int8 [B][heads 64] at S_ctx (*S_ret).  lens: device int32 [B], tokens in the cache
    (the new one included), at most max_len; a sequence of length 0 yields 0.  Key j is visible if j < lens[b] and

@@ -115,7 +115,8 @@ def lib():
         L.ibert_qkv_rope_i8.argtypes = [vp, C.POINTER(RopeDesc), vp, i64, vp, i32, vp, vp, vp, vp, vp]
         L.ibert_attention_decode_i8.argtypes = [vp, vp, vp, vp, vp, vp, i32, i32, i32, i64, i32, i32, i32, i32, i32, dbl, dbl, dbl,
                                                 dbl, i32, vp, vp]
-        for name in ("ibert_kv_slots", "ibert_rope_frequencies", "ibert_rope_rows", "ibert_qkv_rope_i8", "ibert_attention_decode_i8"):
+        L.ibert_attention_window_i8.argtypes = [vp, vp, vp, i32, i32, i64, i32, i32, i32, i32, dbl, dbl, dbl, dbl, i32, vp, vp]
+        for name in ("ibert_attention_window_i8", "ibert_kv_slots", "ibert_rope_frequencies", "ibert_rope_rows", "ibert_qkv_rope_i8", "ibert_attention_decode_i8"):
             getattr(L, name).restype = i32
         for name in ("ibert_create", "ibert_destroy", "ibert_last_status", "ibert_dyadic_from_double",
                      "ibert_linear_i8", "ibert_linear_gelu_i8", "ibert_linear_layernorm_i8", "ibert_softmax_i", "ibert_gelu_i",
@@ -546,6 +547,22 @@ class Context:
                                      _dev(out, torch.int8), _dev(slots, torch.int32), _dev(k_cache, torch.int8),
                                      _dev(v_cache, torch.int8), S_ret), "ibert_qkv_rope_i8")
         return out, tuple(S_ret)
+
+    def ibert_attention_window_i8(self, qkv: torch.Tensor, cu_seqlens: torch.Tensor, max_len: int, heads: int, kv_heads: int,
+                                  S_q: float, S_k: float, S_v: float, S_ctx: float, window: int = 0, sinks: int = 0,
+                                  p_max: int = 255, out: torch.Tensor | None = None):
+        """Causal attention of packed prompts, with a sliding window and sinks; ``qkv`` int8 [tokens, (heads + 2 kv_heads) * 64],
+        ``cu_seqlens`` device int32 [B + 1]."""
+        T = qkv.numel() // ((heads + 2 * kv_heads) * 64)
+        assert qkv.numel() == T * (heads + 2 * kv_heads) * 64
+        if out is None:
+            out = qkv.new_empty((T, heads * 64))
+        assert out.numel() == T * heads * 64
+        S_ret = C.c_double()
+        _chk(lib().ibert_attention_window_i8(self.h, _dev(qkv, torch.int8), _dev(cu_seqlens, torch.int32), cu_seqlens.numel() - 1,
+                                             max_len, T, heads, kv_heads, window, sinks, S_q, S_k, S_v, S_ctx, p_max,
+                                             _dev(out, torch.int8), C.byref(S_ret)), "ibert_attention_window_i8")
+        return out, S_ret.value
 
     def ibert_attention_decode_i8(self, q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, block_tables: torch.Tensor,
                                   lens: torch.Tensor, max_len: int, heads: int, S_q: float, S_k: float, S_v: float, S_ctx: float,

@@ -1210,6 +1210,26 @@ static int check_long_attention(int64_t max_len, int heads, int kv_heads, int wi
   return IBERT_OK;
 }
 
+int ibert_attention_window_i8(ibert_ctx* ctx, const int8_t* qkv, const int32_t* cu_seqlens, int B, int max_len,
+                              int64_t total_tokens, int heads, int kv_heads, int window, int sinks, double S_q, double S_k,
+                              double S_v, double S_ctx, int p_max, int8_t* out, double* S_ret) {
+  return guarded([&]() -> int {
+  if (!ctx || B < 0 || total_tokens < 0) return IBERT_ERR_ARG;
+  int rc = check_long_attention(max_len, heads, kv_heads, window, sinks);
+  if (rc) return rc;
+  if (total_tokens >= (int64_t(1) << 31) - 256 || B >= 1 << 30) return IBERT_ERR_SHAPE;
+  if (B > 0 && total_tokens > 0 && (!qkv || !cu_seqlens || !out)) return IBERT_ERR_ARG;
+  if (!aligned16(qkv) || !aligned16(out) || !aligned4(cu_seqlens)) return IBERT_ERR_ALIGN;
+  LongAttnConsts k{};
+  if ((rc = make_long_attn_consts(S_q, S_k, S_v, S_ctx, p_max, &k))) return rc;
+  if (S_ret) *S_ret = S_ctx;
+  if (B == 0 || total_tokens == 0) return IBERT_OK;
+  DeviceGuard guard(ctx->device);
+  ProfileScope ps(ctx, IBERT_K_ATTENTION);
+  return launch_attention_window(ctx, qkv, cu_seqlens, B, max_len, total_tokens, heads, kv_heads, window, sinks, k, out);
+  });
+}
+
 int ibert_attention_decode_i8(ibert_ctx* ctx, const int8_t* q, const int8_t* k_cache, const int8_t* v_cache,
                               const int32_t* block_tables, const int32_t* lens, int B, int max_len, int max_pages,
                               int64_t n_pages, int page_size, int heads, int kv_heads, int window, int sinks, double S_q,

@@ -93,7 +93,7 @@ attention_decode_kernel(const __grid_constant__ DecodeArgs a) {
   ptx::grid_dep_wait();
 
   // ---- visible keys: j < first and start <= j < len, in tiles of 32: `lead` tiles in front of the window's first one
-  int32_t len = __ldg(a.lens + batch);
+  int32_t len = ptx::ld_dep(a.lens + batch);
   bool bad = len < 0 || len > a.max_len;
   len = min(max(len, 0), a.max_len);
   const int start = a.window > 0 ? max(len - a.window, 0) : 0, first = min(a.sinks, start);
@@ -105,14 +105,14 @@ attention_decode_kernel(const __grid_constant__ DecodeArgs a) {
   auto first_key = [&](int i) { return (i < lead ? i : i - lead + tile_w) * kTile; };
   // offset of row `key` of this kv head in either cache; -1: no such page
   auto row_at = [&](int key) -> int64_t {
-    const int32_t page = __ldg(table + (key >> a.log_page));
+    const int32_t page = ptx::ld_dep(table + (key >> a.log_page));
     if ((uint32_t)page >= (uint32_t)a.n_pages) return -1;
     return ((int64_t)page * a.kv_heads + kvh) * head_bytes + (int64_t)(key & ((1 << a.log_page) - 1)) * kHeadDim;
   };
   auto seen = [&](int key) { return key < len && (key >= start || key < first); };
 
   uint4 q = make_uint4(0, 0, 0, 0);
-  if (g < G) q = __ldg(reinterpret_cast<const uint4*>(a.q + ((int64_t)batch * a.heads + head0 + g) * kHeadDim) + t);
+  if (g < G) q = ptx::ld_dep(reinterpret_cast<const uint4*>(a.q + ((int64_t)batch * a.heads + head0 + g) * kHeadDim) + t);
 
   // ---- scores of this CTA's tiles, and their maximum
   constexpr int32_t kNone = INT32_MIN;

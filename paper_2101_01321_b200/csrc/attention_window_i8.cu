@@ -1,0 +1,377 @@
+// Integer-only causal attention of packed sequences with a sliding window and first tokens that stay visible.
+//
+// Per (query, head), over its visible keys:  s_j = q k_j,  M = max s_j,  e_j = i-exp(M - s_j) (Algorithm 3),
+//   w_j = (e_j b_w + 2^23) >> 24  (u8, p_max at the maximum),  O = sum w_j v_j,  W = sum w_j,  out = O / W at S_ctx
+// -- the definition of the paged attention (attention_decode_i8.cu), so a token's context is the same whether it is
+// computed here with its prompt or there alone.
+//
+// i-exp needs the row's maximum before the first exponential (its shifts do not commute with a later maximum), so the
+// scores are computed twice: pass A takes the maximum of all score tiles, pass B recomputes them, weights them and
+// multiplies with V.  The second Q K^T costs the tensor pipe 64 of the 1400 clocks that the exponentials of a tile take;
+// in exchange O is never rescaled and accumulates in tensor memory as exact integers.
+//
+// A CTA takes 128 consecutive ROWS of the packed tensor, whatever sequences they belong to, and one head: keys run from
+// the first row's first visible key to the last row, each row with bounds of its own.  So short sequences share tiles,
+// and the grid follows from the row count alone.  128 threads, thread = query row = TMEM lane; four CTAs per SM (128
+// columns of tensor memory each: 64 scores, 64 context values; pass A, which has no context yet, takes 128 scores at a
+// time) hide each other's waits.
+#include <cuda.h>
+
+#include <algorithm>
+
+#include "device_utils.cuh"
+#include "sm100_ptx.cuh"
+
+namespace ibert {
+namespace {
+
+constexpr int kWinThreads = 128;
+constexpr int kKeys = 64;                          // keys per tile
+constexpr int kSlot = kKeys * kHeadDim;            // 4 KB
+constexpr int kWinSmem = 128 * kHeadDim + 4 * kSlot + 2 * kSlot + 128 * kKeys + 128 + 1024;
+
+struct WindowArgs {
+  const int32_t* cu;                               // [B + 1]
+  int8_t* out;                                     // [T][heads 64]
+  int32_t* status;
+  int32_t T, B, max_len, heads, kv_heads, window, sinks, tiles;
+  int32_t int_min;                                 // INT32_MIN, as a run-time value (see add_alu)
+  LongAttnConsts k;
+};
+
+// 64-bit mask of the bits [a, b) with a, b clamped to [0, 64]
+__device__ __forceinline__ uint64_t bits_between(int a, int b) {
+  a = min(max(a, 0), 64);
+  b = min(max(b, 0), 64);
+  const uint64_t below_b = b == 64 ? ~0ull : (1ull << b) - 1ull, below_a = a == 64 ? ~0ull : (1ull << a) - 1ull;
+  return below_b & ~below_a;
+}
+// bytes of 255 where bit i of the low four is set
+__device__ __forceinline__ uint32_t byte_mask(uint32_t m) { return ((m & 15u) * 0x00204081u & 0x01010101u) * 255u; }
+
+// MODE: how i-exp is evaluated; 0: folded without a pre-shift, 1: folded with one, 2: the wide form
+template <int MODE>
+__global__ void __launch_bounds__(kWinThreads, 4)
+attention_window_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_kv,
+                        const __grid_constant__ WindowArgs a) {
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint8_t* sQ = smem;                              // [128][64 B], 64-byte swizzle
+  uint8_t* sK = sQ + 128 * kHeadDim;               // two pairs of tiles [64][64 B], 64-byte swizzle
+  uint8_t* sV = sK + 4 * kSlot;                    // two tiles
+  uint8_t* sP = sV + 2 * kSlot;                    // [128][64 B], 64-byte swizzle
+  uint64_t* s_bar = reinterpret_cast<uint64_t*>(sP + 128 * kKeys);
+  const uint32_t bar_q = ptx::smem_addr(s_bar), bar_k = bar_q + 8, bar_v = bar_q + 24, bar_s = bar_q + 40, bar_pv = bar_q + 48;
+  uint32_t* s_tmem = reinterpret_cast<uint32_t*>(s_bar + 7);
+  int32_t* s_bounds = reinterpret_cast<int32_t*>(s_bar + 8);   // first visible key, first row of the sequence, last row's first key
+
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int head = (int)blockIdx.x % a.heads;
+  const int q0 = (a.tiles - 1 - (int)blockIdx.x / a.heads) * 128;       // the rows with most keys first
+  if (warp == 0) {
+    if (ptx::elect_one()) {
+      ptx::mbar_init(bar_q, 1);
+      for (int i = 0; i < 2; ++i) {
+        ptx::mbar_init(bar_k + 8 * i, 1);
+        ptx::mbar_init(bar_v + 8 * i, 1);
+      }
+      ptx::mbar_init(bar_s, 1);
+      ptx::mbar_init(bar_pv, 1);
+      ptx::fence_mbar_init();
+      ptx::tma_prefetch_desc(&map_q);
+      ptx::tma_prefetch_desc(&map_kv);
+    }
+    __syncwarp();
+    ptx::tmem_alloc(ptx::smem_addr(s_tmem), 128);
+    ptx::tmem_relinquish();
+  }
+  ptx::grid_dep_launch();
+  ptx::grid_dep_wait();
+
+  // ---- this row's sequence: the last b with cu[b] <= row, searched 32-fold for the warp's first row, on from there
+  const int row = min(q0 + tid, a.T - 1);
+  int lo_b = 0, hi_b = a.B;
+  const int row_w = min(q0 + warp * 32, a.T - 1);
+  while (hi_b - lo_b > 1) {
+    const int step = (hi_b - lo_b + 31) / 32, i = lo_b + lane * step;
+    const uint32_t le = __ballot_sync(0xffffffffu, i < hi_b && (lane == 0 || ptx::ld_dep(a.cu + i) <= row_w));
+    const int n = __popc(le & ~(le + 1)) ;                   // leading run of ones from lane 0
+    lo_b += (n - 1) * step;
+    hi_b = min(lo_b + step, hi_b);
+  }
+  for (int step = 1; lo_b + 1 < a.B && ptx::ld_dep(a.cu + lo_b + 1) <= row;) {           // (other rows of the warp: gallop)
+    if (lo_b + step < a.B && ptx::ld_dep(a.cu + lo_b + step) <= row) { lo_b += step; step <<= 1; }
+    else step = max(step >> 1, 1);
+  }
+  const int c0 = ptx::ld_dep(a.cu + lo_b), c1 = ptx::ld_dep(a.cu + lo_b + 1);
+  const bool real = q0 + tid < a.T && row >= c0 && row < c1;
+  const int first = real ? max(c0, 0) : row;                 // of the sequence; a row of none sees itself and is not stored
+  const int low = max(first, row - (a.window > 0 ? a.window : a.max_len) + 1);
+  const bool bad = real && c1 - c0 > a.max_len;
+  if (tid == 0) { s_bounds[0] = low; s_bounds[1] = first; }
+  if (tid == 127) s_bounds[2] = low;
+  ptx::tc_fence_before_sync();
+  const bool any = __syncthreads_or(real);
+  ptx::tc_fence_after_sync();
+  const uint32_t tmem = *s_tmem, t_row = tmem + ((uint32_t)(warp * 32) << 16);
+  const int key_w = s_bounds[0], seq0 = s_bounds[1], low_last = s_bounds[2];
+
+  // ---- tiles of 64 keys: `lead` over the sinks of the first row's sequence, then from the first row's window on
+  const int sink_end = a.window > 0 ? (int)min((int64_t)seq0 + a.sinks, (int64_t)key_w) : seq0;
+  const int lead = any ? (sink_end - seq0 + kKeys - 1) / kKeys : 0;
+  const int nt = any ? lead + (min(q0 + 128, a.T) - key_w + kKeys - 1) / kKeys : 0, np = (nt + 1) / 2;
+  auto base_of = [&](int i) { return i < lead ? seq0 + i * kKeys : key_w + (i - lead) * kKeys; };
+  auto mask_of = [&](int i) {
+    const int j0 = base_of(i);
+    const int sinks_end = (int)min((int64_t)first + a.sinks, (int64_t)row + 1);
+    if (i < lead) return bits_between(first - j0, min(sinks_end, key_w) - j0);
+    uint64_t m = bits_between(low - j0, row + 1 - j0);
+    if (a.window > 0) m |= bits_between(first - j0, sinks_end - j0);
+    return m;
+  };
+  auto whole = [&](int i) { return i >= lead && base_of(i) >= low_last && base_of(i) + kKeys - 1 <= q0; };
+
+  const int kvh = head / (a.heads / a.kv_heads);
+  const int col_k = (a.heads + kvh) * kHeadDim, col_v = col_k + a.kv_heads * kHeadDim;
+  int k_loads = 0, v_loads = 0;                    // (warp 0) pairs of K tiles and V tiles requested
+  auto load_k = [&](int s) {                       // pair s of pass A, then of pass B
+    const int i = 2 * (s < np ? s : s - np);
+    const uint32_t bar = bar_k + 8 * (s & 1), dst = ptx::smem_addr(sK) + (s & 1) * 2 * kSlot;
+    ptx::mbar_arrive_expect_tx(bar, i + 1 < nt ? 2 * kSlot : kSlot);
+    ptx::tma_load_2d(dst, &map_kv, bar, col_k, base_of(i));
+    if (i + 1 < nt) ptx::tma_load_2d(dst + kSlot, &map_kv, bar, col_k, base_of(i + 1));
+  };
+  auto load_v = [&](int i) {
+    ptx::mbar_arrive_expect_tx(bar_v + 8 * (i & 1), kSlot);
+    ptx::tma_load_2d(ptx::smem_addr(sV) + (i & 1) * kSlot, &map_kv, bar_v + 8 * (i & 1), col_v, base_of(i));
+  };
+  const uint64_t dq = ptx::make_kmajor_desc(ptx::smem_addr(sQ), 512, ptx::kSwizzle64);
+  auto score_mma = [&](uint32_t k_addr, int n) {   // S = Q K^T over n keys: 64 dimensions are two K steps
+    const uint32_t idesc = ptx::make_idesc_i8(128, n, true, true);
+    const uint64_t dk = ptx::make_kmajor_desc(k_addr, 512, ptx::kSwizzle64);
+    ptx::mma_i8_ss(tmem, dq, dk, idesc, 0u);
+    ptx::mma_i8_ss(tmem, dq + 2, dk + 2, idesc, 1u);
+    ptx::mma_commit(bar_s);
+  };
+
+  bool ok = true;
+  if (nt > 0 && warp == 0) {
+    if (ptx::elect_one()) {
+      ptx::mbar_arrive_expect_tx(bar_q, 128 * kHeadDim);
+      ptx::tma_load_2d(ptx::smem_addr(sQ), &map_q, bar_q, head * kHeadDim, q0);
+      load_k(0);
+      load_k(1);
+      load_v(0);
+    }
+    k_loads = 2;
+    v_loads = 1;
+    ok = __all_sync(0xffffffffu, ptx::mbar_wait(bar_q, 0));
+  }
+
+  // ---- pass A: row maxima, 128 keys at a time
+  int32_t mx = INT32_MIN;
+  uint32_t s_phase = 0;
+  for (int p = 0; p < np; ++p) {
+    if (warp == 0) {
+      if (ok) ok = __all_sync(0xffffffffu, ptx::mbar_wait(bar_k + 8 * (p & 1), (p >> 1) & 1));
+      if (ok && ptx::elect_one()) {
+        ptx::tc_fence_after_sync();
+        score_mma(ptx::smem_addr(sK) + (p & 1) * 2 * kSlot, 2 * p + 1 < nt ? 128 : 64);
+      }
+      __syncwarp();
+    }
+    if (ok) ok = __all_sync(0xffffffffu, ptx::mbar_wait(bar_s, s_phase));
+    s_phase ^= 1;
+    if (warp == 0 && ok && p + 2 < 2 * np) {
+      if (ptx::elect_one()) load_k(p + 2);
+      __syncwarp();
+      k_loads = p + 3;
+    }
+    if (ok) {
+      ptx::tc_fence_after_sync();
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int i = 2 * p + h;
+        if (i < nt) {
+          uint32_t v[64];
+          ptx::tmem_ld64(t_row + h * kKeys, v);
+          ptx::tmem_wait_ld();
+          if (!whole(i)) {
+            const uint64_t m = mask_of(i);
+            const uint32_t m0 = (uint32_t)m, m1 = (uint32_t)(m >> 32);
+#pragma unroll
+            for (int j = 0; j < 64; ++j)
+              if (!(((j < 32 ? m0 : m1) >> (j & 31)) & 1u)) v[j] = (uint32_t)INT32_MIN;
+          }
+#pragma unroll
+          for (int j = 0; j < 64; j += 2) mx = __vimax3_s32(mx, (int32_t)v[j], (int32_t)v[j + 1]);
+        }
+      }
+    }
+    ptx::tc_fence_before_sync();
+    ok = __syncthreads_and(ok);
+    if (!ok) break;
+  }
+
+  // ---- pass B: weights, O = sum w v
+  const LongAttnConsts& k = a.k;
+  const ExpConsts& ek = k.e;
+  const int64_t mk = iexp_folded_addend(ek);
+  const int32_t neg_m = -(int32_t)ek.fold_m, wk = iexp_folded_offset(ek, mx);
+  auto weight = [&](uint32_t s) {                  // w in the upper byte
+    uint32_t e;
+    if constexpr (MODE == 0) e = iexp_folded(add_alu((int32_t)s, wk, a.int_min), mk, neg_m, ek.q_ln2, ek.q_c);
+    else if constexpr (MODE == 1) e = iexp_folded((int32_t)(s + (uint32_t)wk) >> ek.s_in, mk, neg_m, ek.q_ln2, ek.q_c);
+    else e = iexp_dist_wide((uint32_t)mx - s, ek);
+    return e * k.b_w + (1u << 23);
+  };
+  uint32_t sum = 0;
+  if (nt > 0 && ok && warp == 0) {
+    ok = __all_sync(0xffffffffu, ptx::mbar_wait(bar_k + 8 * (np & 1), (np >> 1) & 1));
+    if (ok && ptx::elect_one()) {
+      ptx::tc_fence_after_sync();
+      score_mma(ptx::smem_addr(sK) + (np & 1) * 2 * kSlot, 64);
+    }
+    __syncwarp();
+  }
+  for (int i = 0; i < nt; ++i) {
+    uint32_t v[64];
+    if (ok) ok = __all_sync(0xffffffffu, ptx::mbar_wait(bar_s, s_phase));
+    s_phase ^= 1;
+    if (ok) {
+      ptx::tc_fence_after_sync();
+      ptx::tmem_ld64(t_row, v);
+      ptx::tmem_wait_ld();
+    }
+    ptx::tc_fence_before_sync();
+    ok = __syncthreads_and(ok);                    // every row's scores are in registers
+    if (!ok) break;
+    if (warp == 0) {
+      const int s = np + (i >> 1);                 // pair of tile i; a pair is done with its second (or the last) tile
+      if ((i & 1) && s + 2 < 2 * np) {
+        if (ptx::elect_one()) load_k(s + 2);
+        __syncwarp();
+        k_loads = s + 3;
+      }
+      if (i + 1 < nt) {
+        const int s1 = np + ((i + 1) >> 1);
+        if (!((i + 1) & 1)) ok = __all_sync(0xffffffffu, ptx::mbar_wait(bar_k + 8 * (s1 & 1), (s1 >> 1) & 1));
+        if (ok && ptx::elect_one()) {
+          ptx::tc_fence_after_sync();
+          score_mma(ptx::smem_addr(sK) + (s1 & 1) * 2 * kSlot + ((i + 1) & 1) * kSlot, 64);
+        }
+        __syncwarp();
+      }
+    }
+    uint32_t w[16];
+#pragma unroll
+    for (int j = 0; j < 16; ++j)
+      w[j] = __byte_perm(__byte_perm(weight(v[4 * j]), weight(v[4 * j + 1]), 0x0073),
+                         __byte_perm(weight(v[4 * j + 2]), weight(v[4 * j + 3]), 0x0073), 0x5410);
+    if (!whole(i)) {
+      const uint64_t m = mask_of(i);
+#pragma unroll
+      for (int j = 0; j < 16; ++j) w[j] &= byte_mask((uint32_t)(m >> (4 * j)));
+    }
+#pragma unroll
+    for (int j = 0; j < 16; ++j) sum = __dp4a(w[j], 0x01010101u, sum);
+    if (i > 0) {                                   // the product before has read P and its V
+      if (ok) ok = __all_sync(0xffffffffu, ptx::mbar_wait(bar_pv, (i - 1) & 1));
+    }
+    if (warp == 0 && ok && i + 1 < nt) {
+      if (ptx::elect_one()) load_v(i + 1);
+      __syncwarp();
+      v_loads = i + 2;
+    }
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+      *reinterpret_cast<uint4*>(sP + tid * kKeys + ((c ^ ((tid >> 1) & 3)) << 4)) =
+          make_uint4(w[4 * c], w[4 * c + 1], w[4 * c + 2], w[4 * c + 3]);
+    ptx::fence_proxy_async_smem();
+    if (warp == 0 && ok) ok = __all_sync(0xffffffffu, ptx::mbar_wait(bar_v + 8 * (i & 1), (i >> 1) & 1));
+    ptx::tc_fence_before_sync();
+    ok = __syncthreads_and(ok);                    // P complete
+    if (!ok) break;
+    if (warp == 0) {
+      if (ptx::elect_one()) {
+        ptx::tc_fence_after_sync();
+        const uint32_t idesc = ptx::make_idesc_i8(128, kHeadDim, false, true) | (1u << 16);      // u8 x s8, V MN-major
+        const uint64_t dp = ptx::make_kmajor_desc(ptx::smem_addr(sP), 512, ptx::kSwizzle64);
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk) {
+          const uint32_t va = ptx::smem_addr(sV) + (i & 1) * kSlot + kk * 32 * kHeadDim;
+          const uint64_t dv = (uint64_t)((va & 0x3FFFFu) >> 4) | ((uint64_t)(512 >> 4) << 16) | ((uint64_t)(512 >> 4) << 32) |
+                              ((uint64_t)1 << 46) | ((uint64_t)ptx::kSwizzle64 << 61);
+          ptx::mma_i8_ss(tmem + kKeys, dp + 2 * kk, dv, idesc, i + kk > 0 ? 1u : 0u);
+        }
+        ptx::mma_commit(bar_pv);
+      }
+      __syncwarp();
+    }
+  }
+  if (nt > 0 && ok) ok = __all_sync(0xffffffffu, ptx::mbar_wait(bar_pv, (nt - 1) & 1));
+
+  // ---- the weighted mean of this row
+  if (nt > 0 && ok) {
+    ptx::tc_fence_after_sync();
+    uint32_t v[64];
+    ptx::tmem_ld64(t_row + kKeys, v);
+    ptx::tmem_wait_ld();
+    if (real) {
+      const RowShare share = row_share(sum, k);
+      int8_t* o = a.out + ((int64_t)row * a.heads + head) * kHeadDim;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        uint32_t w[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          w[j] = pack4_sat_s8(weighted_mean((int32_t)v[16 * c + 4 * j], share), weighted_mean((int32_t)v[16 * c + 4 * j + 1], share),
+                              weighted_mean((int32_t)v[16 * c + 4 * j + 2], share), weighted_mean((int32_t)v[16 * c + 4 * j + 3], share));
+        reinterpret_cast<uint4*>(o)[c] = make_uint4(w[0], w[1], w[2], w[3]);
+      }
+    }
+  }
+  if (!ok) {
+    atomicCAS(a.status, 0, IBERT_ERR_TIMEOUT);
+    if (warp == 0) {                               // copies still in flight land before the shared memory is given up
+      for (int s = max(k_loads - 2, 0); s < k_loads; ++s) ptx::mbar_wait(bar_k + 8 * (s & 1), (s >> 1) & 1);
+      for (int i = max(v_loads - 2, 0); i < v_loads; ++i) ptx::mbar_wait(bar_v + 8 * (i & 1), (i >> 1) & 1);
+      ptx::mbar_wait(bar_q, 0);
+    }
+  }
+  if (bad) atomicCAS(a.status, 0, IBERT_ERR_VALUE_RANGE);
+  ptx::tc_fence_before_sync();
+  __syncthreads();
+  if (warp == 0) {
+    ptx::tc_fence_after_sync();
+    ptx::tmem_dealloc(tmem, 128);
+  }
+}
+
+}  // namespace
+
+int launch_attention_window(ibert_ctx* ctx, const int8_t* qkv, const int32_t* cu, int B, int max_len, int64_t T, int heads,
+                            int kv_heads, int window, int sinks, const LongAttnConsts& k, int8_t* out) {
+  const uint64_t cols = (uint64_t)(heads + 2 * kv_heads) * kHeadDim;
+  const uint64_t dims[2] = {cols, (uint64_t)T}, str[1] = {cols};
+  const uint32_t box_q[2] = {kHeadDim, 128}, box_kv[2] = {kHeadDim, kKeys};
+  CUtensorMap mq, mkv;
+  if (int rc = encode_tensor_map(&mq, qkv, 2, dims, str, box_q, 64)) return rc;
+  if (int rc = encode_tensor_map(&mkv, qkv, 2, dims, str, box_kv, 64)) return rc;
+  WindowArgs a{};
+  a.cu = cu; a.out = out; a.status = ctx->d_status;
+  a.T = (int32_t)T; a.B = B; a.max_len = max_len; a.heads = heads; a.kv_heads = kv_heads; a.window = window; a.sinks = sinks;
+  a.tiles = (int32_t)((T + 127) / 128); a.int_min = INT32_MIN; a.k = k;
+  const int64_t grid = (int64_t)a.tiles * heads;
+  if (grid > INT32_MAX) return IBERT_ERR_SHAPE;
+  auto kernel = !iexp_takes_folded(k.e) ? attention_window_kernel<2>
+                : k.e.s_in == 0         ? attention_window_kernel<0>
+                                        : attention_window_kernel<1>;
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kWinSmem) != cudaSuccess) {
+    cudaGetLastError();
+    return IBERT_ERR_CUDA;
+  }
+  return launch_pdl(kernel, dim3((unsigned)grid), dim3(kWinThreads), (size_t)kWinSmem, ctx->stream, 1, mq, mkv, a);
+}
+
+}  // namespace ibert

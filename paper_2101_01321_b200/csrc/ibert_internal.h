@@ -312,6 +312,10 @@ int launch_attention_decode(ibert_ctx* ctx, const int8_t* q, const int8_t* k_cac
                             int max_len, int heads, int kv_heads, int window, int sinks, const LongAttnConsts& k,
                             int8_t* out);
 
+// packed sequences, rows cu[b] .. cu[b+1] - 1 of T; causal, window and sinks
+int launch_attention_window(ibert_ctx* ctx, const int8_t* qkv, const int32_t* cu, int B, int max_len, int64_t T, int heads,
+                            int kv_heads, int window, int sinks, const LongAttnConsts& k, int8_t* out);
+
 constexpr int kMaxRequests = 8192;       // of one launch_kv_slots
 int launch_kv_slots(ibert_ctx* ctx, const int32_t* lens, const int32_t* new_lens, int32_t* tables, int32_t* stack,
                     const int32_t* n_free, int B, int log_page, int max_pages, int64_t capacity, int64_t max_tokens,

@@ -75,7 +75,8 @@ kv_slots_kernel(const SlotArgs a) {
   const uint32_t rank = ptx::cluster_ctarank();
   const int n_cta = (int)gridDim.x;
   bool bad = false;
-  ptx::grid_dep_launch();
+  // (no early start of the next kernel: the packed attention reads row offsets ahead of its dependency wait, and those may
+  // be this kernel's)
   ptx::grid_dep_wait();
 
   const int64_t n_in = *a.n_free;
@@ -89,7 +90,7 @@ kv_slots_kernel(const SlotArgs a) {
   int64_t sum = 0;
   for (int b = b0; b < b1; ++b) {
     int32_t len = a.lens[b];              // (plain loads: what the call writes may lie in the same arrays)
-    const int32_t f = __ldg(a.fresh + b);
+    const int32_t f = ptx::ld_dep(a.fresh + b);
     if (len < 0 || len > most) { bad = true; len = len < 0 ? 0 : (int32_t)most; }
     s_len[b] = f < 0 ? -1 - len : len;
     sum += max(f, 0);
@@ -104,7 +105,7 @@ kv_slots_kernel(const SlotArgs a) {
   sum = 0;
   for (int b = b0; b < b1; ++b) {
     s_tok[b] = (int32_t)before;
-    const int32_t f = max(__ldg(a.fresh + b), 0);
+    const int32_t f = max(ptx::ld_dep(a.fresh + b), 0);
     const int64_t next = add_capped(before, f);
     const int32_t held = s_len[b];
     if (held < 0) sum += (int64_t)pages(-1 - held) << 32;

@@ -57,15 +57,15 @@ qkv_rope_kernel(const __grid_constant__ RopeArgs a) {
   bool bad = false;
   int32_t cs[4];                                             // (cos, sin) of the lane's four pairs
   if (rotates) {
-    int32_t pos = __ldg(a.positions + t);
+    int32_t pos = ptx::ld_dep(a.positions + t);
     if (pos < 0 || pos >= a.max_pos) { bad = true; pos = 0; }
-    const int4 w = __ldg(reinterpret_cast<const int4*>(a.rope + (int64_t)pos * a.rot) + lane8);
+    const int4 w = ptx::ld_dep(reinterpret_cast<const int4*>(a.rope + (int64_t)pos * a.rot) + lane8);
     cs[0] = w.x; cs[1] = w.y; cs[2] = w.z; cs[3] = w.w;
   }
   int8_t* cache_row = nullptr;                               // first byte of head 0's row in the K cache
   int64_t v_minus_k = 0;
   if (a.k_cache) {
-    const int32_t slot = __ldg(a.slots + t);
+    const int32_t slot = ptx::ld_dep(a.slots + t);
     if (slot >= 0 && slot < a.n_slots) {
       const int64_t page = slot >> a.log_page, row = slot & ((1 << a.log_page) - 1);
       cache_row = a.k_cache + (((page * a.kv_heads) << a.log_page) + row) * kHeadDim;

@@ -35,6 +35,10 @@ __device__ __forceinline__ bool elect_one() {
 // still reads.  grid_dep_launch() lets the next kernel of the stream be scheduled early.
 // Both are no-ops for a kernel launched the ordinary way.
 __device__ __forceinline__ void grid_dep_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+// A load of what an earlier kernel of the stream may have written, behind grid_dep_wait().  Not __ldg: the compiler takes
+// that for a load of constant memory and may move it in front of the wait, where the writer may still be running.
+template <typename T>
+__device__ __forceinline__ T ld_dep(const T* p) { return *p; }
 __device__ __forceinline__ void grid_dep_launch() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
 // ------------------------------------------------------------------ mbarrier

@@ -87,6 +87,27 @@ def test_attention_decode_refuses(lib, kw, code):
     assert _decode(lib, **kw) == code
 
 
+def _window(lib, **kw):
+    a = dict(ctx=CTX, qkv=P16, cu=P16, B=2, max_len=100, T=50, heads=4, kv_heads=2, window=0, sinks=0, S_q=0.05, S_k=0.05, S_v=0.05,
+             S_ctx=0.02, p_max=255, out=P16, S_ret=None) | kw
+    return lib.ibert_attention_window_i8(*a.values())
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(ctx=None), ARG), (dict(B=-1), ARG), (dict(T=-1), ARG), (dict(window=-1), ARG), (dict(sinks=-1), ARG), (dict(p_max=1), ARG),
+    (dict(qkv=None), ARG), (dict(cu=None), ARG), (dict(out=None), ARG), (dict(max_len=0), SHAPE), (dict(max_len=65537), SHAPE),
+    (dict(max_len=70000, window=65000, sinks=537), SHAPE), (dict(heads=0), SHAPE), (dict(heads=5), SHAPE), (dict(kv_heads=0), SHAPE),
+    (dict(T=(1 << 31) - 256), SHAPE), (dict(S_k=0.0), SCALE), (dict(S_q=1.5, S_k=1.4), SCALE), (dict(S_v=float("nan")), SCALE),
+    (dict(qkv=P16 + 8), ALIGN), (dict(out=P16 + 8), ALIGN), (dict(cu=P16 + 2), ALIGN)])
+def test_attention_window_refuses(lib, kw, code):
+    assert _window(lib, **kw) == code
+
+
+def test_no_rows_are_no_work(lib):
+    assert _window(lib, T=0, qkv=None, out=None) == 0
+    assert _window(lib, B=0, T=5) == 0
+
+
 # ----------------------------------------------------------------------------- rotation tables
 @pytest.mark.parametrize("rot", [8, 16, 48, 64])
 @pytest.mark.parametrize("pos0,n,factor", [(0, 50, 1.0), (131000, 9, 1.0), (7, 3, 1.37), (5, 0, 1.0)])
