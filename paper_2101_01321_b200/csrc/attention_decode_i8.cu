@@ -8,15 +8,16 @@
 // hundred keys of similar score every floor(e p_max / sum) would be 0.
 //
 // i-exp is defined from the row's maximum and its shifts do not commute with a later, larger one, so the sequence is
-// split over a CLUSTER of CTAs instead of over independent blocks: every CTA keeps the scores of its keys in shared
-// memory, the maxima meet through distributed shared memory, then every CTA weights its values, and the partial
-// O and W (whole numbers, so no order matters) are summed by the CTAs of the cluster, each a part of the 64 dimensions.
-// K and V are read once; nothing but the result is written.
+// split over a CLUSTER of CTAs instead of over independent blocks: every CTA finds the maximum of its keys' scores, the
+// maxima meet through distributed shared memory, then every CTA weights its values, and the partial O and W (whole
+// numbers, so no order matters) are summed by the CTAs of the cluster, each a part of the results.  Nothing but the result
+// is written.
 //
-// The products run on mma.sync m16n8k32 (s8 x s8, s8 x u8): eight query heads of a group are the n of a tile, and the
-// kernel is bound by the 128 bytes per key, not by the tensor pipe.  A lane's 16 bytes of a key are the A operand of
-// both k steps as they come (any order of the 64 dimensions will do if Q has the same); the values of four keys are
-// transposed in registers by byte permutes.
+// The products run on mma.sync m16n8k32 (s8 x s8, s8 x u8): up to eight query heads of a group, and the kernel is bound by
+// the 128 bytes per key and the instructions around them, not by the tensor pipe.  S^T = Q K^T leaves a lane with one head
+// and the very keys whose weights it needs as the B operand of O^T = V^T w; the 16 bytes of a key that a lane copies are
+// the operand of both K steps as they come (any order of the 64 dimensions will do if Q has the same); the values of four
+// keys are transposed in registers by byte permutes.
 #include <algorithm>
 
 #include "device_utils.cuh"
@@ -25,9 +26,10 @@
 namespace ibert {
 namespace {
 
-constexpr int kDecThreads = 256, kDecWarps = kDecThreads / 32;
 constexpr int kTile = 32;                // keys a warp takes at a time
+constexpr int kTileBytes = kTile * kHeadDim;
 constexpr int kMaxGroup = 8;             // query heads per CTA
+constexpr int kMaxCluster = 16;
 
 struct DecodeArgs {
   const int8_t *q, *k_cache, *v_cache;
@@ -36,7 +38,7 @@ struct DecodeArgs {
   int32_t* status;
   int32_t heads, kv_heads, group, tiles_of_group;     // query heads per kv head, and in pieces of kMaxGroup
   int32_t log_page, max_pages, n_pages, max_len, window, sinks;
-  int32_t score_pitch;                   // 32-bit words per head in shared memory, = 16 mod 32
+  int32_t score_pitch;                   // words of scores per head in shared memory, = 16 mod 32
   LongAttnConsts k;
 };
 
@@ -62,18 +64,18 @@ __device__ __forceinline__ void transpose4(const uint32_t* w, uint32_t* o) {
   o[3] = __byte_perm(b, d, 0x7632);
 }
 
-// Where key 4 j + t of a tile lies in its 32 scores: a lane then finds the eight keys t, 4 + t, .. of its weights as two
-// runs of four words
-__device__ __forceinline__ int score_place(int key) {
-  const int t = key & 3, j = key >> 2;
-  return ((j >> 2) << 4) + (t << 2) + (j & 3);
-}
-
-__global__ void __launch_bounds__(kDecThreads)
+// W warps with STAGES tiles of each in flight.  KEEP: the scores stay in shared memory from the maximum to the weights, and the
+// exponentials of a head are spread over all threads; else the keys are read a second time (out of L2) and every lane computes
+// the weights that it needs itself.  For one or two heads the eight weights per lane and tile would be those of an eighth or a
+// quarter of the lanes; for more, the scores' 4 bytes per head and key take the shared memory that the loads in flight need.
+template <int W, int STAGES, bool KEEP>
+__global__ void __launch_bounds__(32 * W, KEEP ? 4 : 2)
 attention_decode_kernel(const __grid_constant__ DecodeArgs a) {
-  extern __shared__ int32_t s_score[];                        // [heads of this CTA][score_pitch]
-  __shared__ int32_t s_all_max[16][kMaxGroup];                // by CTA of the cluster
-  __shared__ int32_t s_warp_max[kDecWarps][kMaxGroup];
+  constexpr int kThreads = 32 * W;
+  extern __shared__ __align__(16) uint8_t smem[];
+  int32_t* s_score = reinterpret_cast<int32_t*>(smem + W * STAGES * kTileBytes);               // KEEP: [heads][score_pitch]
+  __shared__ int32_t s_all_max[kMaxCluster][kMaxGroup];       // by CTA of the cluster
+  __shared__ int32_t s_warp_max[W][kMaxGroup];
   __shared__ int32_t s_out[kMaxGroup][kHeadDim];              // partial O
   __shared__ int32_t s_sum[kMaxGroup];                        // partial W
 
@@ -83,11 +85,10 @@ attention_decode_kernel(const __grid_constant__ DecodeArgs a) {
   asm("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(cl));
   const int item = (int)blockIdx.x / cl;
   const int piece = item % a.tiles_of_group, pair = item / a.tiles_of_group;
-  const int kvh = pair % a.kv_heads, batch = pair / a.kv_heads;
-  const int head0 = kvh * a.group + piece * kMaxGroup;
-  const int G = min(a.group - piece * kMaxGroup, kMaxGroup);  // query heads of this CTA
+  const int kvh = pair % a.kv_heads;
+  const int batch = pair / a.kv_heads;
 
-  for (int i = tid; i < kMaxGroup * kHeadDim; i += kDecThreads) (&s_out[0][0])[i] = 0;
+  for (int i = tid; i < kMaxGroup * kHeadDim; i += kThreads) (&s_out[0][0])[i] = 0;
   if (tid < kMaxGroup) s_sum[tid] = 0;
   ptx::grid_dep_launch();
   ptx::grid_dep_wait();
@@ -100,129 +101,200 @@ attention_decode_kernel(const __grid_constant__ DecodeArgs a) {
   const int tile_w = start / kTile, lead = min((first + kTile - 1) / kTile, tile_w);
   const int tiles = len > 0 ? lead + (len + kTile - 1) / kTile - tile_w : 0;
   const int per = (tiles + cl - 1) / cl, i0 = min((int)rank * per, tiles), i1 = min(i0 + per, tiles);
-  const int32_t* table = a.tables + (int64_t)batch * a.max_pages;
-  const int64_t head_bytes = (int64_t)kHeadDim << a.log_page;
+  const int head0 = kvh * a.group + piece * kMaxGroup;
+  const int G = min(a.group - piece * kMaxGroup, kMaxGroup);  // query heads of this CTA
   auto first_key = [&](int i) { return (i < lead ? i : i - lead + tile_w) * kTile; };
-  // offset of row `key` of this kv head in either cache; -1: no such page
-  auto row_at = [&](int key) -> int64_t {
-    const int32_t page = ptx::ld_dep(table + (key >> a.log_page));
-    if ((uint32_t)page >= (uint32_t)a.n_pages) return -1;
-    return ((int64_t)page * a.kv_heads + kvh) * head_bytes + (int64_t)(key & ((1 << a.log_page) - 1)) * kHeadDim;
-  };
   auto seen = [&](int key) { return key < len && (key >= start || key < first); };
-
-  uint4 q = make_uint4(0, 0, 0, 0);
+  // Byte offsets in either cache of keys 0 and 16 of every tile of this CTA.  A page holds whole halves of tiles, and rows of
+  // it past the sequence's end may be read as well as any.  Bit 0: some of the half's keys are not visible; bit 1: none is, or
+  // there is no such page (the offset is then page 0's, which may be read too: the scores are masked, the weights 0).
+  int64_t* s_place = reinterpret_cast<int64_t*>(s_score + (KEEP ? G * a.score_pitch : 0));
+  for (int i = tid; i < 2 * (i1 - i0); i += kThreads) {
+    const int key0 = first_key(i0 + (i >> 1)) + 16 * (i & 1);
+    int64_t place = 3;
+    if (key0 < len && (key0 + 15 >= start || key0 < first)) {
+      const int32_t page = ptx::ld_dep(a.tables + (int64_t)batch * a.max_pages + (key0 >> a.log_page));
+      if ((uint32_t)page < (uint32_t)a.n_pages) {
+        const bool whole = key0 + 16 <= len && (key0 >= start || key0 + 16 <= first);
+        place = ((((int64_t)page * a.kv_heads + kvh) << a.log_page) + (key0 & ((1 << a.log_page) - 1))) * kHeadDim + (whole ? 0 : 1);
+      } else bad = true;
+    }
+    s_place[i] = place;
+  }
+  uint4 q = make_uint4(0, 0, 0, 0);      // 16 bytes of head g, the A operand's rows 0 to 7 (rows 8 to 15 are zeros)
   if (g < G) q = ptx::ld_dep(reinterpret_cast<const uint4*>(a.q + ((int64_t)batch * a.heads + head0 + g) * kHeadDim) + t);
+  __syncthreads();                       // s_place, s_out and s_sum are filled
 
-  // ---- scores of this CTA's tiles, and their maximum
+  // ---- a warp's stream of tiles, copied into a ring of its own: its keys, then its values (KEEP), or its keys, then a tile of
+  // keys and its values in turn.  The first of the second part are on their way while the CTAs meet.
+  uint8_t* ring = smem + warp * STAGES * kTileBytes;
+  const int n_tiles = i0 + warp < i1 ? (i1 - i0 - warp + W - 1) / W : 0, n_stream = (KEEP ? 2 : 3) * n_tiles;
+  // In a tile of keys, row n of eight is key (n & 1) 4 + (n >> 1): the two keys of a score fragment's lane t are then t and
+  // 4 + t, and the four lanes of a head read the values of four consecutive keys
+  const int k_lane = (((g & 1) << 2) + (g >> 1)) * kHeadDim + t * 16, v_lane = lane * 16;
+  auto issue = [&](int n) {              // tile n of the stream; a lane copies 16 bytes of each of its eight rows
+    if (n < n_stream) {
+      const int m = n - n_tiles, i = n < n_tiles ? n : (KEEP ? m : m >> 1);
+      const bool keys = n < n_tiles || (!KEEP && !(m & 1));
+      const longlong2 p = *reinterpret_cast<const longlong2*>(s_place + 2 * (warp + i * W));
+      const int8_t* base = keys ? a.k_cache + k_lane : a.v_cache + v_lane;
+      const int8_t *lo = base + (p.x & ~int64_t(3)), *hi = base + (p.y & ~int64_t(3));
+      const uint32_t dst = ptx::smem_addr(ring + (n & (STAGES - 1)) * kTileBytes + lane * 16);
+      ptx::cp_async_16(dst, lo);
+      ptx::cp_async_16(dst + 512, lo + 512);
+      ptx::cp_async_16(dst + 1024, hi);
+      ptx::cp_async_16(dst + 1536, hi + 512);
+    }
+    ptx::cp_async_commit();
+  };
   constexpr int32_t kNone = INT32_MIN;
-  int32_t mx0 = kNone, mx1 = kNone;                           // of heads 2t and 2t + 1
-  for (int i = i0 + warp; i < i1; i += kDecWarps) {
-    const int key0 = first_key(i);
-    int32_t* s_tile = s_score + (i - i0) * kTile;
-    uint4 r[4];
-    uint32_t ok = 0;
+  // scores of head g against keys 8 j + t and 8 j + 4 + t (c[j][0], c[j][1]) of a tile of keys that this lane copied itself
+  auto scores = [&](int n, int i, int32_t (&c)[4][4]) {
+    const uint8_t* tile = ring + (n & (STAGES - 1)) * kTileBytes + lane * 16;
 #pragma unroll
-    for (int m = 0; m < 4; ++m) {
-      const int key = key0 + 8 * m + g;
-      r[m] = make_uint4(0, 0, 0, 0);
-      if (seen(key)) {
-        const int64_t at = row_at(key);
-        if (at >= 0) {
-          r[m] = __ldcs(reinterpret_cast<const uint4*>(a.k_cache + at) + t);
-          ok |= 1u << m;
-        } else bad = true;
-      }
+    for (int j = 0; j < 4; ++j) {
+      const uint4 r = *reinterpret_cast<const uint4*>(tile + j * 512);
+      c[j][0] = c[j][1] = c[j][2] = c[j][3] = 0;
+      mma_s8(c[j], q.x, 0u, q.y, 0u, r.x, r.y);
+      mma_s8(c[j], q.z, 0u, q.w, 0u, r.z, r.w);
     }
+    const int2 flags = make_int2((int)s_place[2 * (warp + i * W)] & 3, (int)s_place[2 * (warp + i * W) + 1] & 3);
+    if (flags.x | flags.y) {
+      const int key0 = first_key(i0 + warp + i * W) + t;
 #pragma unroll
-    for (int m = 0; m < 2; ++m) {
-      int32_t c[4] = {0, 0, 0, 0};
-      mma_s8(c, r[2 * m].x, r[2 * m + 1].x, r[2 * m].y, r[2 * m + 1].y, q.x, q.y);
-      mma_s8(c, r[2 * m].z, r[2 * m + 1].z, r[2 * m].w, r[2 * m + 1].w, q.z, q.w);
+      for (int j = 0; j < 4; ++j)
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {                           // keys 16 m + g and 16 m + 8 + g
-        const int place = score_place(16 * m + 8 * h + g);
-        const bool there = (ok >> (2 * m + h)) & 1;
-        const int32_t v0 = there ? c[2 * h] : kNone, v1 = there ? c[2 * h + 1] : kNone;
-        mx0 = max(mx0, v0);
-        mx1 = max(mx1, v1);
-        if (2 * t < G) s_tile[2 * t * a.score_pitch + place] = v0;
-        if (2 * t + 1 < G) s_tile[(2 * t + 1) * a.score_pitch + place] = v1;
-      }
+        for (int e = 0; e < 2; ++e)
+          if (((j < 2 ? flags.x : flags.y) & 2) || !seen(key0 + 8 * j + 4 * e)) c[j][e] = kNone;
+    }
+  };
+#pragma unroll
+  for (int n = 0; n < STAGES; ++n) issue(n);
+
+  // ---- the largest score of every head
+  int32_t mx = kNone;                    // of head g
+  for (int n = 0; n < n_tiles; ++n) {
+    ptx::cp_async_wait<STAGES - 1>();
+    int32_t c[4][4];
+    scores(n, n, c);
+    issue(n + STAGES);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) mx = __vimax3_s32(mx, c[j][0], c[j][1]);
+    if (KEEP && g < G) {                 // four to a later word: keys t, 4 + t, 8 + t, 12 + t and 16 + ..
+      int32_t* s_tile = s_score + g * a.score_pitch + (warp + n * W) * kTile + 4 * t;
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        *reinterpret_cast<int2*>(s_tile + 16 * (j >> 1) + 2 * (j & 1)) = make_int2(c[j][0], c[j][1]);
     }
   }
-#pragma unroll
-  for (int d = 4; d < 32; d <<= 1) {
-    mx0 = max(mx0, __shfl_xor_sync(0xffffffffu, mx0, d));
-    mx1 = max(mx1, __shfl_xor_sync(0xffffffffu, mx1, d));
-  }
-  if (g == 0) {
-    s_warp_max[warp][2 * t] = mx0;
-    s_warp_max[warp][2 * t + 1] = mx1;
-  }
+  mx = max(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
+  mx = max(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
+  if (t == 0) s_warp_max[warp][g] = mx;
   __syncthreads();
-  for (int i = tid; i < cl * kMaxGroup; i += kDecThreads) {   // this CTA's maxima into every CTA of the cluster
+  for (int i = tid; i < cl * kMaxGroup; i += kThreads) {      // this CTA's maxima into every CTA of the cluster
     const int h = i & (kMaxGroup - 1), to = i / kMaxGroup;
     int32_t m = s_warp_max[0][h];
-    for (int w = 1; w < kDecWarps; ++w) m = max(m, s_warp_max[w][h]);
+    for (int w = 1; w < W; ++w) m = max(m, s_warp_max[w][h]);
     ptx::st_cluster_s32(ptx::map_to_cta(ptx::smem_addr(&s_all_max[rank][h]), (uint32_t)to), m);
   }
-  ptx::cluster_sync();
-  int32_t mx = kNone;                                         // of head g
-  for (int c = 0; c < cl; ++c) mx = max(mx, s_all_max[c][g]);
+  if (cl > 1) ptx::cluster_sync(); else __syncthreads();
 
   // ---- weights and O = sum w v
   const LongAttnConsts& k = a.k;
   int32_t acc[4][4] = {};                                     // dims 8g + 2i (+ 1) x heads 2t, 2t + 1
-  uint32_t sum = 0;                                           // W of head g over this lane's keys
-  const int64_t mk = iexp_folded_addend(k.e);
-  const int32_t neg_m = -(int32_t)k.e.fold_m, wk = iexp_folded_offset(k.e, mx);
-  const bool folded = iexp_takes_folded(k.e);
-  for (int i = i0 + warp; i < i1; i += kDecWarps) {
-    const int key0 = first_key(i);
-    const int32_t* s_tile = s_score + (i - i0) * kTile;
-    uint32_t x[8], y[8];
+  auto accumulate = [&](int n, uint32_t w0, uint32_t w1) {    // a tile of values: rows t, 4 + t, .. 28 + t, 8 bytes of each
+    const uint8_t* tile = ring + (n & (STAGES - 1)) * kTileBytes + t * kHeadDim + g * 8;
+    uint32_t x[8], y[8], xt[8], yt[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const int key = key0 + 4 * j + t;
-      uint2 v = make_uint2(0, 0);
-      if (seen(key)) {
-        const int64_t at = row_at(key);
-        if (at >= 0) v = __ldcs(reinterpret_cast<const uint2*>(a.v_cache + at) + g);
-      }
+      const uint2 v = *reinterpret_cast<const uint2*>(tile + j * 4 * kHeadDim);
       x[j] = v.x;
       y[j] = v.y;
     }
-    uint32_t w[2] = {0, 0};
-    if (g < G) {
-#pragma unroll
-      for (int p = 0; p < 2; ++p) {
-        const int4 s4 = *reinterpret_cast<const int4*>(s_tile + g * a.score_pitch + 16 * p + 4 * t);
-        const int32_t s[4] = {s4.x, s4.y, s4.z, s4.w};
-        uint32_t e[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          e[j] = folded ? iexp_folded((int32_t)((uint32_t)s[j] + (uint32_t)wk) >> k.e.s_in, mk, neg_m, k.e.q_ln2, k.e.q_c)
-                        : iexp_dist_wide((uint32_t)mx - (uint32_t)s[j], k.e);
-          e[j] = s[j] == kNone ? 0u : e[j] * k.b_w + (1u << 23);
-        }
-        w[p] = __byte_perm(__byte_perm(e[0], e[1], 0x0073), __byte_perm(e[2], e[3], 0x0073), 0x5410);
-        sum = __dp4a(w[p], 0x01010101u, sum);
-      }
-    }
-    uint32_t xt[8], yt[8];
+    __syncwarp();                        // every lane has read the tile
+    issue(n + STAGES);
     transpose4(x, xt);
     transpose4(x + 4, xt + 4);
     transpose4(y, yt);
     transpose4(y + 4, yt + 4);
-    mma_s8u8(acc[0], xt[0], xt[1], xt[4], xt[5], w[0], w[1]);
-    mma_s8u8(acc[1], xt[2], xt[3], xt[6], xt[7], w[0], w[1]);
-    mma_s8u8(acc[2], yt[0], yt[1], yt[4], yt[5], w[0], w[1]);
-    mma_s8u8(acc[3], yt[2], yt[3], yt[6], yt[7], w[0], w[1]);
+    mma_s8u8(acc[0], xt[0], xt[1], xt[4], xt[5], w0, w1);
+    mma_s8u8(acc[1], xt[2], xt[3], xt[6], xt[7], w0, w1);
+    mma_s8u8(acc[2], yt[0], yt[1], yt[4], yt[5], w0, w1);
+    mma_s8u8(acc[3], yt[2], yt[3], yt[6], yt[7], w0, w1);
+  };
+  auto pack = [](const uint32_t* e) {    // the upper bytes of four words
+    return __byte_perm(__byte_perm(e[0], e[1], 0x0073), __byte_perm(e[2], e[3], 0x0073), 0x5410);
+  };
+  auto second_part = [&](auto exp_of) {  // exp_of(score, maximum, offset of the folded form)
+    if constexpr (KEEP) {
+      const int quads = (i1 - i0) * (kTile / 4);
+      for (int h = 0; h < G; ++h) {
+        int32_t top = kNone;
+        for (int c = 0; c < cl; ++c) top = max(top, s_all_max[c][h]);
+        const int32_t wk = iexp_folded_offset(k.e, top);
+        int32_t* row = s_score + h * a.score_pitch;
+        uint32_t sum = 0;
+        for (int i = tid; i < quads; i += kThreads) {         // the word takes the place of the first of its four scores
+          const int4 s4 = *reinterpret_cast<const int4*>(row + 4 * i);
+          const int32_t s[4] = {s4.x, s4.y, s4.z, s4.w};
+          uint32_t e[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) e[j] = s[j] == kNone ? 0u : exp_of(s[j], top, wk) * k.b_w + (1u << 23);
+          const uint32_t w = pack(e);
+          row[4 * i] = (int32_t)w;
+          sum = __dp4a(w, 0x01010101u, sum);
+        }
+        sum = __reduce_add_sync(0xffffffffu, sum);
+        if (lane == 0 && sum != 0) atomicAdd(&s_sum[h], (int32_t)sum);
+      }
+      __syncthreads();
+      for (int n = n_tiles; n < n_stream; ++n) {
+        ptx::cp_async_wait<STAGES - 1>();
+        __syncwarp();                    // every lane's copies of the tile have landed
+        const int32_t* s_tile = s_score + g * a.score_pitch + (warp + (n - n_tiles) * W) * kTile + 4 * t;
+        accumulate(n, g < G ? (uint32_t)s_tile[0] : 0u, g < G ? (uint32_t)s_tile[16] : 0u);
+      }
+    } else {
+      int32_t top = kNone;               // of head g
+      for (int c = 0; c < cl; ++c) top = max(top, s_all_max[c][g]);
+      const int32_t wk = iexp_folded_offset(k.e, top);
+      uint32_t sum = 0;
+      for (int i = 0; i < n_tiles; ++i) {
+        const int n = n_tiles + 2 * i;
+        ptx::cp_async_wait<STAGES - 1>();
+        int32_t c[4][4];
+        scores(n, i, c);
+        issue(n + STAGES);
+        uint32_t w[2];
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+          uint32_t e[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const int32_t s = c[2 * p + (j >> 1)][j & 1];
+            e[j] = s == kNone ? 0u : exp_of(s, top, wk) * k.b_w + (1u << 23);
+          }
+          w[p] = g < G ? pack(e) : 0u;
+          sum = __dp4a(w[p], 0x01010101u, sum);
+        }
+        ptx::cp_async_wait<STAGES - 1>();
+        __syncwarp();
+        accumulate(n + 1, w[0], w[1]);
+      }
+      sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+      sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+      if (t == 0 && sum != 0) atomicAdd(&s_sum[g], (int32_t)sum);
+    }
+  };
+  if (iexp_takes_folded(k.e)) {
+    const int64_t mk = iexp_folded_addend(k.e);
+    const int32_t neg_m = -(int32_t)k.e.fold_m;
+    second_part([&](int32_t s, int32_t, int32_t wk) {
+      return iexp_folded((int32_t)((uint32_t)s + (uint32_t)wk) >> k.e.s_in, mk, neg_m, k.e.q_ln2, k.e.q_c);
+    });
+  } else {
+    second_part([&](int32_t s, int32_t top, int32_t) { return iexp_dist_wide((uint32_t)top - (uint32_t)s, k.e); });
   }
-  sum += __shfl_xor_sync(0xffffffffu, sum, 1);
-  sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-  if (t == 0 && g < G) atomicAdd(&s_sum[g], (int32_t)sum);
 #pragma unroll
   for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -230,10 +302,10 @@ attention_decode_kernel(const __grid_constant__ DecodeArgs a) {
       const int h = 2 * t + (c & 1);
       if (h < G) atomicAdd(&s_out[h][8 * g + 2 * i + (c >> 1)], acc[i][c]);
     }
-  ptx::cluster_sync();
+  if (cl > 1) ptx::cluster_sync(); else __syncthreads();
 
   // ---- every CTA joins and divides its part of the G x 64 results
-  for (int i = (int)rank * kDecThreads + tid; i < G * kHeadDim; i += cl * kDecThreads) {
+  for (int i = (int)rank * kThreads + tid; i < G * kHeadDim; i += cl * kThreads) {
     const int h = i / kHeadDim, d = i % kHeadDim;
     int32_t o = 0;
     uint32_t total = 0;
@@ -244,7 +316,7 @@ attention_decode_kernel(const __grid_constant__ DecodeArgs a) {
     a.out[((int64_t)batch * a.heads + head0 + h) * kHeadDim + d] = (int8_t)weighted_mean(o, row_share(total, k));
   }
   if (bad) atomicCAS(a.status, 0, IBERT_ERR_VALUE_RANGE);
-  ptx::cluster_sync();                   // nobody leaves while a peer may still read its shared memory
+  if (cl > 1) ptx::cluster_sync();       // nobody leaves while a peer may still read its shared memory
 }
 
 }  // namespace
@@ -257,26 +329,35 @@ int launch_attention_decode(ibert_ctx* ctx, const int8_t* q, const int8_t* k_cac
   a.q = q; a.k_cache = k_cache; a.v_cache = v_cache; a.tables = tables; a.lens = lens; a.out = out; a.status = ctx->d_status;
   a.heads = heads; a.kv_heads = kv_heads; a.group = heads / kv_heads;
   a.tiles_of_group = (a.group + kMaxGroup - 1) / kMaxGroup;
-  a.log_page = log_page; a.max_pages = max_pages; a.n_pages = n_pages; a.max_len = max_len; a.window = window; a.sinks = sinks;
+  a.log_page = log_page; a.max_pages = max_pages; a.n_pages = n_pages;
+  a.max_len = n_pages > 0 ? max_len : 0;               // (without pages there are no keys)
+  a.window = window; a.sinks = sinks;
   a.k = k;
   const int64_t items = (int64_t)B * kv_heads * a.tiles_of_group;
   // tiles of 32 keys that a sequence can have: one more where the window starts inside a tile, and the sinks' own
   int64_t tiles = ((int64_t)max_len + kTile - 1) / kTile;
   if (window > 0) tiles = std::min<int64_t>(tiles, ((int64_t)window + kTile - 1) / kTile + 1 + ((int64_t)sinks + kTile - 1) / kTile);
+  const bool keep = a.group <= 2;
+  const int warps = keep ? 4 : 8, stages = 4;
+  const int rows = keep ? a.group : 0;
+  // (rings, scores, then the places of the tiles' halves)
+  auto smem_of = [&](int c) {
+    const int64_t n = (tiles + c - 1) / c;
+    return (int64_t)warps * stages * kTileBytes + rows * (n * kTile + 16) * 4 + n * 16;
+  };
   int cl = 1;
-  while (cl < 16 && items * cl < 2 * ctx->num_sms && (tiles + cl - 1) / cl > kDecWarps) cl <<= 1;
-  const int rows = std::min(a.group, kMaxGroup);
-  auto smem_of = [&](int c) { return (int64_t)rows * ((tiles + c - 1) / c * kTile + 16) * 4; };
-  while (cl < 16 && smem_of(cl) > 96 * 1024) cl <<= 1;
+  while (cl < kMaxCluster && items * cl < 2 * ctx->num_sms && (tiles + cl - 1) / cl > warps) cl <<= 1;
+  while (cl < kMaxCluster && (smem_of(cl) > 112 * 1024 || (!keep && (tiles + cl - 1) / cl > 64))) cl <<= 1;
   const int64_t smem = smem_of(cl);
-  if (smem > 200 * 1024 || items * cl > INT32_MAX) return IBERT_ERR_SHAPE;
+  if (smem > 224 * 1024 || items * cl > INT32_MAX) return IBERT_ERR_SHAPE;
   a.score_pitch = (int32_t)((tiles + cl - 1) / cl * kTile + 16);
-  if (cudaFuncSetAttribute(attention_decode_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 * 1024) != cudaSuccess ||
-      cudaFuncSetAttribute(attention_decode_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) {
+  auto kernel = keep ? attention_decode_kernel<4, 4, true> : attention_decode_kernel<8, 4, false>;
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 224 * 1024) != cudaSuccess ||
+      cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) {
     cudaGetLastError();
     return IBERT_ERR_CUDA;
   }
-  return launch_pdl(attention_decode_kernel, dim3((unsigned)(items * cl)), dim3(kDecThreads), (size_t)smem, ctx->stream, cl, a);
+  return launch_pdl(kernel, dim3((unsigned)(items * cl)), dim3(32 * warps), (size_t)smem, ctx->stream, cl, a);
 }
 
 }  // namespace ibert

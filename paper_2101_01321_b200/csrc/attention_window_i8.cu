@@ -12,7 +12,7 @@
 //
 // A CTA takes 128 consecutive ROWS of the packed tensor, whatever sequences they belong to, and one head: keys run from
 // the first row's first visible key to the last row, each row with bounds of its own.  So short sequences share tiles,
-// and the grid follows from the row count alone.  128 threads, thread = query row = TMEM lane; four CTAs per SM (128
+// and the grid follows from the row count alone.  256 threads, two per query row (= TMEM lane); four CTAs per SM (128
 // columns of tensor memory each: 64 scores, 64 context values; pass A, which has no context yet, takes 128 scores at a
 // time) hide each other's waits.
 #include <cuda.h>
@@ -25,10 +25,10 @@
 namespace ibert {
 namespace {
 
-constexpr int kWinThreads = 128;
+constexpr int kWinThreads = 256;                  // two per query row
 constexpr int kKeys = 64;                          // keys per tile
 constexpr int kSlot = kKeys * kHeadDim;            // 4 KB
-constexpr int kWinSmem = 128 * kHeadDim + 4 * kSlot + 2 * kSlot + 128 * kKeys + 128 + 1024;
+constexpr int kWinSmem = 128 * kHeadDim + 4 * kSlot + 2 * kSlot + 128 * kKeys + 128 + 2 * 128 * 4 + 1024;
 
 struct WindowArgs {
   const int32_t* cu;                               // [B + 1]
@@ -64,8 +64,10 @@ attention_window_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
   const uint32_t bar_q = ptx::smem_addr(s_bar), bar_k = bar_q + 8, bar_v = bar_q + 24, bar_s = bar_q + 40, bar_pv = bar_q + 48;
   uint32_t* s_tmem = reinterpret_cast<uint32_t*>(s_bar + 7);
   int32_t* s_bounds = reinterpret_cast<int32_t*>(s_bar + 8);   // first visible key, first row of the sequence, last row's first key
+  int32_t* s_join = s_bounds + 8;                  // [2][128] what the two threads of a row exchange
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int half = tid >> 7, r = tid & 127;        // half of the columns, row in the tile (= TMEM lane)
   const int head = (int)blockIdx.x % a.heads;
   const int q0 = (a.tiles - 1 - (int)blockIdx.x / a.heads) * 128;       // the rows with most keys first
   if (warp == 0) {
@@ -89,9 +91,9 @@ attention_window_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
   ptx::grid_dep_wait();
 
   // ---- this row's sequence: the last b with cu[b] <= row, searched 32-fold for the warp's first row, on from there
-  const int row = min(q0 + tid, a.T - 1);
+  const int row = min(q0 + r, a.T - 1);
   int lo_b = 0, hi_b = a.B;
-  const int row_w = min(q0 + warp * 32, a.T - 1);
+  const int row_w = min(q0 + (warp & 3) * 32, a.T - 1);
   while (hi_b - lo_b > 1) {
     const int step = (hi_b - lo_b + 31) / 32, i = lo_b + lane * step;
     const uint32_t le = __ballot_sync(0xffffffffu, i < hi_b && (lane == 0 || ptx::ld_dep(a.cu + i) <= row_w));
@@ -104,16 +106,16 @@ attention_window_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
     else step = max(step >> 1, 1);
   }
   const int c0 = ptx::ld_dep(a.cu + lo_b), c1 = ptx::ld_dep(a.cu + lo_b + 1);
-  const bool real = q0 + tid < a.T && row >= c0 && row < c1;
+  const bool real = q0 + r < a.T && row >= c0 && row < c1;
   const int first = real ? max(c0, 0) : row;                 // of the sequence; a row of none sees itself and is not stored
   const int low = max(first, row - (a.window > 0 ? a.window : a.max_len) + 1);
   const bool bad = real && c1 - c0 > a.max_len;
   if (tid == 0) { s_bounds[0] = low; s_bounds[1] = first; }
-  if (tid == 127) s_bounds[2] = low;
+  if (tid == 127) s_bounds[2] = low;       // (of the tile's last row)
   ptx::tc_fence_before_sync();
   const bool any = __syncthreads_or(real);
   ptx::tc_fence_after_sync();
-  const uint32_t tmem = *s_tmem, t_row = tmem + ((uint32_t)(warp * 32) << 16);
+  const uint32_t tmem = *s_tmem, t_row = tmem + ((uint32_t)((warp & 3) * 32) << 16);
   const int key_w = s_bounds[0], seq0 = s_bounds[1], low_last = s_bounds[2];
 
   // ---- tiles of 64 keys: `lead` over the sinks of the first row's sequence, then from the first row's window on
@@ -189,22 +191,22 @@ attention_window_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
     }
     if (ok) {
       ptx::tc_fence_after_sync();
+      const int i = 2 * p + half;                  // half of the threads takes each of the pair's tiles
+      if (i < nt) {
+        const uint64_t m = whole(i) ? ~0ull : mask_of(i);
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int i = 2 * p + h;
-        if (i < nt) {
-          uint32_t v[64];
-          ptx::tmem_ld64(t_row + h * kKeys, v);
+        for (int c = 0; c < 2; ++c) {
+          uint32_t v[32];
+          ptx::tmem_ld32(t_row + half * kKeys + c * 32, v);
           ptx::tmem_wait_ld();
-          if (!whole(i)) {
-            const uint64_t m = mask_of(i);
-            const uint32_t m0 = (uint32_t)m, m1 = (uint32_t)(m >> 32);
+          const uint32_t mc = (uint32_t)(m >> (32 * c));
+          if (__any_sync(0xffffffffu, mc != 0xffffffffu)) {
 #pragma unroll
-            for (int j = 0; j < 64; ++j)
-              if (!(((j < 32 ? m0 : m1) >> (j & 31)) & 1u)) v[j] = (uint32_t)INT32_MIN;
+            for (int j = 0; j < 32; ++j)
+              if (!((mc >> j) & 1u)) v[j] = (uint32_t)INT32_MIN;
           }
 #pragma unroll
-          for (int j = 0; j < 64; j += 2) mx = __vimax3_s32(mx, (int32_t)v[j], (int32_t)v[j + 1]);
+          for (int j = 0; j < 32; j += 2) mx = __vimax3_s32(mx, (int32_t)v[j], (int32_t)v[j + 1]);
         }
       }
     }
@@ -212,6 +214,10 @@ attention_window_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
     ok = __syncthreads_and(ok);
     if (!ok) break;
   }
+
+  s_join[tid] = mx;
+  __syncthreads();
+  mx = max(s_join[r], s_join[128 + r]);
 
   // ---- pass B: weights, O = sum w v
   const LongAttnConsts& k = a.k;
@@ -235,12 +241,12 @@ attention_window_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
     __syncwarp();
   }
   for (int i = 0; i < nt; ++i) {
-    uint32_t v[64];
+    uint32_t v[32];
     if (ok) ok = __all_sync(0xffffffffu, ptx::mbar_wait(bar_s, s_phase));
     s_phase ^= 1;
     if (ok) {
       ptx::tc_fence_after_sync();
-      ptx::tmem_ld64(t_row, v);
+      ptx::tmem_ld32(t_row + 32 * half, v);
       ptx::tmem_wait_ld();
     }
     ptx::tc_fence_before_sync();
@@ -263,18 +269,18 @@ attention_window_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
         __syncwarp();
       }
     }
-    uint32_t w[16];
+    uint32_t w[8];
 #pragma unroll
-    for (int j = 0; j < 16; ++j)
+    for (int j = 0; j < 8; ++j)
       w[j] = __byte_perm(__byte_perm(weight(v[4 * j]), weight(v[4 * j + 1]), 0x0073),
                          __byte_perm(weight(v[4 * j + 2]), weight(v[4 * j + 3]), 0x0073), 0x5410);
     if (!whole(i)) {
-      const uint64_t m = mask_of(i);
+      const uint32_t m = (uint32_t)(mask_of(i) >> (32 * half));
 #pragma unroll
-      for (int j = 0; j < 16; ++j) w[j] &= byte_mask((uint32_t)(m >> (4 * j)));
+      for (int j = 0; j < 8; ++j) w[j] &= byte_mask(m >> (4 * j));
     }
 #pragma unroll
-    for (int j = 0; j < 16; ++j) sum = __dp4a(w[j], 0x01010101u, sum);
+    for (int j = 0; j < 8; ++j) sum = __dp4a(w[j], 0x01010101u, sum);
     if (i > 0) {                                   // the product before has read P and its V
       if (ok) ok = __all_sync(0xffffffffu, ptx::mbar_wait(bar_pv, (i - 1) & 1));
     }
@@ -284,8 +290,8 @@ attention_window_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
       v_loads = i + 2;
     }
 #pragma unroll
-    for (int c = 0; c < 4; ++c)
-      *reinterpret_cast<uint4*>(sP + tid * kKeys + ((c ^ ((tid >> 1) & 3)) << 4)) =
+    for (int c = 0; c < 2; ++c)
+      *reinterpret_cast<uint4*>(sP + r * kKeys + (((2 * half + c) ^ ((r >> 1) & 3)) << 4)) =
           make_uint4(w[4 * c], w[4 * c + 1], w[4 * c + 2], w[4 * c + 3]);
     ptx::fence_proxy_async_smem();
     if (warp == 0 && ok) ok = __all_sync(0xffffffffu, ptx::mbar_wait(bar_v + 8 * (i & 1), (i >> 1) & 1));
@@ -311,17 +317,21 @@ attention_window_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
   }
   if (nt > 0 && ok) ok = __all_sync(0xffffffffu, ptx::mbar_wait(bar_pv, (nt - 1) & 1));
 
-  // ---- the weighted mean of this row
+  // ---- the weighted mean of this row, 32 dimensions per thread
+  __syncthreads();                                 // (the maxima have been read)
+  s_join[tid] = (int32_t)sum;
+  __syncthreads();
+  sum = (uint32_t)s_join[r] + (uint32_t)s_join[128 + r];
   if (nt > 0 && ok) {
     ptx::tc_fence_after_sync();
-    uint32_t v[64];
-    ptx::tmem_ld64(t_row + kKeys, v);
+    uint32_t v[32];
+    ptx::tmem_ld32(t_row + kKeys + 32 * half, v);
     ptx::tmem_wait_ld();
     if (real) {
       const RowShare share = row_share(sum, k);
-      int8_t* o = a.out + ((int64_t)row * a.heads + head) * kHeadDim;
+      int8_t* o = a.out + ((int64_t)row * a.heads + head) * kHeadDim + 32 * half;
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
+      for (int c = 0; c < 2; ++c) {
         uint32_t w[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j)

@@ -13,6 +13,7 @@
 namespace ibert {
 namespace {
 
+
 constexpr int kSlotThreads = 1024;
 
 struct SlotArgs {
@@ -20,7 +21,7 @@ struct SlotArgs {
   int32_t* tables;                  // [B][max_pages]
   int32_t* stack;                   // free pages, `*n_free` of them
   const int32_t* n_free;
-  int32_t B, log_page, max_pages;
+  int32_t B, log_page, max_pages, run;     // run: tokens a thread takes one after the other
   int64_t capacity, max_tokens;
   int32_t *lens_out, *n_free_out, *cu, *slots, *positions;
   int32_t* status;
@@ -171,21 +172,34 @@ kv_slots_kernel(const SlotArgs a) {
     const int b = owner(s_need, B, k);
     a.tables[(int64_t)b * a.max_pages + pages(s_len[b]) + (k - s_need[b])] = taken(k);
   }
-  for (int64_t i = t0; i < a.max_tokens; i += step) {
-    int32_t slot = -1, pos = 0;
-    if (i < total_tokens) {
-      const int b = owner(s_tok, B, (int32_t)i);
-      const int32_t held = s_len[b], had = pages(held);
-      const int64_t p = held + (i - s_tok[b]);
-      const int32_t j = (int32_t)(p >> a.log_page);
-      const int32_t page = p >= most ? -1
-                           : j < had ? a.tables[(int64_t)b * a.max_pages + j] : taken(s_need[b] + j - had);
-      const int64_t s = ((int64_t)page << a.log_page) + (p & (P - 1));
-      if (page >= 0 && s <= INT32_MAX) slot = (int32_t)s; else bad = true;
-      pos = p < most ? (int32_t)p : 0;
+  // tokens in runs: the request is searched and a page looked up once per run, and again where they change
+  for (int64_t i0 = (int64_t)t0 * a.run; i0 < a.max_tokens; i0 += (int64_t)step * a.run) {
+    int b = -1;
+    int32_t page = -1, page_at = -1;
+    for (int u = 0; u < a.run; ++u) {
+      const int64_t i = i0 + u;
+      int32_t slot = -1, pos = 0;
+      if (i < total_tokens) {
+        if (b < 0 || i >= s_tok[b + 1]) {
+          b = owner(s_tok, B, (int32_t)i);
+          page_at = -1;
+        }
+        const int32_t held = s_len[b], had = pages(held);
+        const int64_t p = held + (i - s_tok[b]);
+        const int32_t j = (int32_t)(p >> a.log_page);
+        if (j != page_at) {
+          page = p >= most ? -1 : j < had ? a.tables[(int64_t)b * a.max_pages + j] : taken(s_need[b] + j - had);
+          page_at = j;
+        }
+        const int64_t s = ((int64_t)page << a.log_page) + (p & (P - 1));
+        if (page >= 0 && s <= INT32_MAX) slot = (int32_t)s; else bad = true;
+        pos = p < most ? (int32_t)p : 0;
+      }
+      if (i < a.max_tokens) {
+        a.slots[i] = slot;
+        a.positions[i] = pos;
+      }
     }
-    a.slots[i] = slot;
-    a.positions[i] = pos;
   }
   if (bad) atomicCAS(a.status, 0, IBERT_ERR_VALUE_RANGE);
 }
@@ -195,15 +209,15 @@ kv_slots_kernel(const SlotArgs a) {
 int launch_kv_slots(ibert_ctx* ctx, const int32_t* lens, const int32_t* new_lens, int32_t* tables, int32_t* stack,
                     const int32_t* n_free, int B, int log_page, int max_pages, int64_t capacity, int64_t max_tokens,
                     int32_t* lens_out, int32_t* n_free_out, int32_t* cu, int32_t* slots, int32_t* positions) {
-  SlotArgs a{lens, new_lens, tables, stack, n_free, B, log_page, max_pages, capacity, max_tokens,
+  const int ctas = max_tokens <= 4096 ? 1 : 8;
+  const int run = max_tokens <= (int64_t)ctas * kSlotThreads ? 1 : 4;
+  SlotArgs a{lens, new_lens, tables, stack, n_free, B, log_page, max_pages, run, capacity, max_tokens,
              lens_out, n_free_out, cu, slots, positions, ctx->d_status};
   const size_t smem = (4 * (size_t)B + 3) * sizeof(int32_t);
-  if (smem > 40 * 1024 &&
-      cudaFuncSetAttribute(kv_slots_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) {
+  if (smem > 40 * 1024 && cudaFuncSetAttribute(kv_slots_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) {
     cudaGetLastError();
     return IBERT_ERR_CUDA;
   }
-  const int ctas = 1;
   return launch_pdl(kv_slots_kernel, dim3(ctas), dim3(kSlotThreads), smem, ctx->stream, ctas, a);
 }
 
