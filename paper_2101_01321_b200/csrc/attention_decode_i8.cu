@@ -29,7 +29,8 @@ namespace {
 constexpr int kTile = 32;                // keys a warp takes at a time
 constexpr int kTileBytes = kTile * kHeadDim;
 constexpr int kMaxGroup = 8;             // query heads per CTA
-constexpr int kMaxCluster = 16;
+constexpr int kMaxCluster = 8;           // (larger ones find no place on the GPU for long: 16 x 32768 x 32 heads 55 us at 16, 37 at 8)
+constexpr int kDecMaxSmem = 160 * 1024;
 
 struct DecodeArgs {
   const int8_t *q, *k_cache, *v_cache;
@@ -42,6 +43,13 @@ struct DecodeArgs {
   LongAttnConsts k;
 };
 
+// the same on accumulators of zeros
+__device__ __forceinline__ void mma_s8_first(int32_t (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                             uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+               : "=r"(c[0]), "=r"(c[1]), "=r"(c[2]), "=r"(c[3])
+               : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "r"(0));
+}
 __device__ __forceinline__ void mma_s8(int32_t (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
                                        uint32_t b1) {
   asm volatile("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
@@ -69,14 +77,14 @@ __device__ __forceinline__ void transpose4(const uint32_t* w, uint32_t* o) {
 // the weights that it needs itself.  For one or two heads the eight weights per lane and tile would be those of an eighth or a
 // quarter of the lanes; for more, the scores' 4 bytes per head and key take the shared memory that the loads in flight need.
 template <int W, int STAGES, bool KEEP>
-__global__ void __launch_bounds__(32 * W, KEEP ? 4 : 2)
+__global__ void __launch_bounds__(32 * W, KEEP ? 5 : 3)
 attention_decode_kernel(const __grid_constant__ DecodeArgs a) {
   constexpr int kThreads = 32 * W;
   extern __shared__ __align__(16) uint8_t smem[];
   int32_t* s_score = reinterpret_cast<int32_t*>(smem + W * STAGES * kTileBytes);               // KEEP: [heads][score_pitch]
   __shared__ int32_t s_all_max[kMaxCluster][kMaxGroup];       // by CTA of the cluster
   __shared__ int32_t s_warp_max[W][kMaxGroup];
-  __shared__ int32_t s_out[kMaxGroup][kHeadDim];              // partial O
+  __shared__ int32_t s_out[16][32];      // partial O: [4 i + c][lane] holds head 2 t + (c & 1), dimension 8 g + 2 i + (c >> 1)
   __shared__ int32_t s_sum[kMaxGroup];                        // partial W
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
@@ -148,14 +156,14 @@ attention_decode_kernel(const __grid_constant__ DecodeArgs a) {
     ptx::cp_async_commit();
   };
   constexpr int32_t kNone = INT32_MIN;
-  // scores of head g against keys 8 j + t and 8 j + 4 + t (c[j][0], c[j][1]) of a tile of keys that this lane copied itself
+  // scores of head g against keys 8 j + t and 8 j + 4 + t (c[j][0], c[j][1]) of a tile of keys that this lane copied itself,
+  // and whether some of them are masked
   auto scores = [&](int n, int i, int32_t (&c)[4][4]) {
     const uint8_t* tile = ring + (n & (STAGES - 1)) * kTileBytes + lane * 16;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const uint4 r = *reinterpret_cast<const uint4*>(tile + j * 512);
-      c[j][0] = c[j][1] = c[j][2] = c[j][3] = 0;
-      mma_s8(c[j], q.x, 0u, q.y, 0u, r.x, r.y);
+      mma_s8_first(c[j], q.x, 0u, q.y, 0u, r.x, r.y);
       mma_s8(c[j], q.z, 0u, q.w, 0u, r.z, r.w);
     }
     const int2 flags = make_int2((int)s_place[2 * (warp + i * W)] & 3, (int)s_place[2 * (warp + i * W) + 1] & 3);
@@ -167,6 +175,7 @@ attention_decode_kernel(const __grid_constant__ DecodeArgs a) {
         for (int e = 0; e < 2; ++e)
           if (((j < 2 ? flags.x : flags.y) & 2) || !seen(key0 + 8 * j + 4 * e)) c[j][e] = kNone;
     }
+    return (flags.x | flags.y) != 0;
   };
 #pragma unroll
   for (int n = 0; n < STAGES; ++n) issue(n);
@@ -263,7 +272,7 @@ attention_decode_kernel(const __grid_constant__ DecodeArgs a) {
         const int n = n_tiles + 2 * i;
         ptx::cp_async_wait<STAGES - 1>();
         int32_t c[4][4];
-        scores(n, i, c);
+        const bool masked = scores(n, i, c);
         issue(n + STAGES);
         uint32_t w[2];
 #pragma unroll
@@ -271,8 +280,12 @@ attention_decode_kernel(const __grid_constant__ DecodeArgs a) {
           uint32_t e[4];
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            const int32_t s = c[2 * p + (j >> 1)][j & 1];
-            e[j] = s == kNone ? 0u : exp_of(s, top, wk) * k.b_w + (1u << 23);
+            e[j] = exp_of(c[2 * p + (j >> 1)][j & 1], top, wk) * k.b_w + (1u << 23);
+          }
+          if (masked) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              if (c[2 * p + (j >> 1)][j & 1] == kNone) e[j] = 0u;
           }
           w[p] = g < G ? pack(e) : 0u;
           sum = __dp4a(w[p], 0x01010101u, sum);
@@ -289,28 +302,30 @@ attention_decode_kernel(const __grid_constant__ DecodeArgs a) {
   if (iexp_takes_folded(k.e)) {
     const int64_t mk = iexp_folded_addend(k.e);
     const int32_t neg_m = -(int32_t)k.e.fold_m;
-    second_part([&](int32_t s, int32_t, int32_t wk) {
-      return iexp_folded((int32_t)((uint32_t)s + (uint32_t)wk) >> k.e.s_in, mk, neg_m, k.e.q_ln2, k.e.q_c);
-    });
+    if (k.e.s_in == 0)
+      second_part([&](int32_t s, int32_t, int32_t wk) { return iexp_folded((int32_t)((uint32_t)s + (uint32_t)wk), mk, neg_m, k.e.q_ln2, k.e.q_c); });
+    else
+      second_part([&](int32_t s, int32_t, int32_t wk) {
+        return iexp_folded((int32_t)((uint32_t)s + (uint32_t)wk) >> k.e.s_in, mk, neg_m, k.e.q_ln2, k.e.q_c);
+      });
   } else {
     second_part([&](int32_t s, int32_t top, int32_t) { return iexp_dist_wide((uint32_t)top - (uint32_t)s, k.e); });
   }
 #pragma unroll
   for (int i = 0; i < 4; ++i)
 #pragma unroll
-    for (int c = 0; c < 4; ++c) {
-      const int h = 2 * t + (c & 1);
-      if (h < G) atomicAdd(&s_out[h][8 * g + 2 * i + (c >> 1)], acc[i][c]);
-    }
+    for (int c = 0; c < 4; ++c)
+      if (2 * t + (c & 1) < G) atomicAdd(&s_out[4 * i + c][lane], acc[i][c]);
   if (cl > 1) ptx::cluster_sync(); else __syncthreads();
 
   // ---- every CTA joins and divides its part of the G x 64 results
   for (int i = (int)rank * kThreads + tid; i < G * kHeadDim; i += cl * kThreads) {
     const int h = i / kHeadDim, d = i % kHeadDim;
+    const int32_t* part = &s_out[((d & 7) >> 1) * 4 + ((d & 1) << 1) + (h & 1)][(d >> 3) * 4 + (h >> 1)];
     int32_t o = 0;
     uint32_t total = 0;
     for (int c = 0; c < cl; ++c) {
-      o += ptx::ld_cluster_s32(ptx::map_to_cta(ptx::smem_addr(&s_out[h][d]), (uint32_t)c));
+      o += ptx::ld_cluster_s32(ptx::map_to_cta(ptx::smem_addr(part), (uint32_t)c));
       total += (uint32_t)ptx::ld_cluster_s32(ptx::map_to_cta(ptx::smem_addr(&s_sum[h]), (uint32_t)c));
     }
     a.out[((int64_t)batch * a.heads + head0 + h) * kHeadDim + d] = (int8_t)weighted_mean(o, row_share(total, k));
@@ -338,7 +353,7 @@ int launch_attention_decode(ibert_ctx* ctx, const int8_t* q, const int8_t* k_cac
   int64_t tiles = ((int64_t)max_len + kTile - 1) / kTile;
   if (window > 0) tiles = std::min<int64_t>(tiles, ((int64_t)window + kTile - 1) / kTile + 1 + ((int64_t)sinks + kTile - 1) / kTile);
   const bool keep = a.group <= 2;
-  const int warps = keep ? 4 : 8, stages = 4;
+  const int warps = keep ? 4 : 8, stages = keep ? 4 : 2;
   const int rows = keep ? a.group : 0;
   // (rings, scores, then the places of the tiles' halves)
   auto smem_of = [&](int c) {
@@ -347,15 +362,19 @@ int launch_attention_decode(ibert_ctx* ctx, const int8_t* q, const int8_t* k_cac
   };
   int cl = 1;
   while (cl < kMaxCluster && items * cl < 2 * ctx->num_sms && (tiles + cl - 1) / cl > warps) cl <<= 1;
-  while (cl < kMaxCluster && (smem_of(cl) > 112 * 1024 || (!keep && (tiles + cl - 1) / cl > 64))) cl <<= 1;
+  while (cl < kMaxCluster && smem_of(cl) > 112 * 1024) cl <<= 1;
   const int64_t smem = smem_of(cl);
-  if (smem > 224 * 1024 || items * cl > INT32_MAX) return IBERT_ERR_SHAPE;
+  if (smem > kDecMaxSmem || items * cl > INT32_MAX) return IBERT_ERR_SHAPE;
   a.score_pitch = (int32_t)((tiles + cl - 1) / cl * kTile + 16);
-  auto kernel = keep ? attention_decode_kernel<4, 4, true> : attention_decode_kernel<8, 4, false>;
-  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 224 * 1024) != cudaSuccess ||
-      cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) {
-    cudaGetLastError();
-    return IBERT_ERR_CUDA;
+  auto kernel = keep ? attention_decode_kernel<4, 4, true> : attention_decode_kernel<8, 2, false>;
+  static bool set[kMaxDevices][2] = {{false}};
+  bool& done = set[ctx->device % kMaxDevices][keep ? 1 : 0];
+  if (!done) {
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kDecMaxSmem) != cudaSuccess) {
+      cudaGetLastError();
+      return IBERT_ERR_CUDA;
+    }
+    done = true;
   }
   return launch_pdl(kernel, dim3((unsigned)(items * cl)), dim3(32 * warps), (size_t)smem, ctx->stream, cl, a);
 }

@@ -12,7 +12,8 @@
 //
 // A CTA takes 128 consecutive ROWS of the packed tensor, whatever sequences they belong to, and one head: keys run from
 // the first row's first visible key to the last row, each row with bounds of its own.  So short sequences share tiles,
-// and the grid follows from the row count alone.  256 threads, two per query row (= TMEM lane); four CTAs per SM (128
+// and the grid follows from the row count alone.  Four warps, a thread per query row (= TMEM lane), and one that issues
+// copies and products; four CTAs per SM (128
 // columns of tensor memory each: 64 scores, 64 context values; pass A, which has no context yet, takes 128 scores at a
 // time) hide each other's waits.
 #include <cuda.h>
@@ -25,10 +26,11 @@
 namespace ibert {
 namespace {
 
-constexpr int kWinThreads = 256;                  // two per query row
+constexpr int kWinThreads = 160;                   // four warps of rows, one that feeds the tensor pipe
 constexpr int kKeys = 64;                          // keys per tile
 constexpr int kSlot = kKeys * kHeadDim;            // 4 KB
-constexpr int kWinSmem = 128 * kHeadDim + 4 * kSlot + 2 * kSlot + 128 * kKeys + 128 + 2 * 128 * 4 + 1024;
+constexpr int kP = 128 * kKeys;                    // weights of a tile: 8 KB
+constexpr int kWinSmem = 128 * kHeadDim + 4 * kSlot + 2 * kSlot + 2 * kP + 256 + 1024;
 
 struct WindowArgs {
   const int32_t* cu;                               // [B + 1]
@@ -59,15 +61,15 @@ attention_window_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
   uint8_t* sQ = smem;                              // [128][64 B], 64-byte swizzle
   uint8_t* sK = sQ + 128 * kHeadDim;               // two pairs of tiles [64][64 B], 64-byte swizzle
   uint8_t* sV = sK + 4 * kSlot;                    // two tiles
-  uint8_t* sP = sV + 2 * kSlot;                    // [128][64 B], 64-byte swizzle
-  uint64_t* s_bar = reinterpret_cast<uint64_t*>(sP + 128 * kKeys);
-  const uint32_t bar_q = ptx::smem_addr(s_bar), bar_k = bar_q + 8, bar_v = bar_q + 24, bar_s = bar_q + 40, bar_pv = bar_q + 48;
-  uint32_t* s_tmem = reinterpret_cast<uint32_t*>(s_bar + 7);
-  int32_t* s_bounds = reinterpret_cast<int32_t*>(s_bar + 8);   // first visible key, first row of the sequence, last row's first key
-  int32_t* s_join = s_bounds + 8;                  // [2][128] what the two threads of a row exchange
+  uint8_t* sP = sV + 2 * kSlot;                    // two of [128][64 B], 64-byte swizzle
+  uint64_t* s_bar = reinterpret_cast<uint64_t*>(sP + 2 * kP);
+  const uint32_t bar_q = ptx::smem_addr(s_bar), bar_k = bar_q + 8, bar_v = bar_q + 24;       // copies: Q, pairs of K tiles, V tiles
+  const uint32_t bar_s = bar_q + 40, bar_free = bar_q + 48;          // scores complete; scores read by the four warps
+  const uint32_t bar_p = bar_q + 56, bar_pv = bar_q + 72;            // weights written (two buffers); their product done
+  uint32_t* s_tmem = reinterpret_cast<uint32_t*>(s_bar + 11);
+  int32_t* s_bounds = reinterpret_cast<int32_t*>(s_bar + 12);  // first visible key, first row of the sequence, last row's first key
 
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int half = tid >> 7, r = tid & 127;        // half of the columns, row in the tile (= TMEM lane)
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, r = tid & 127;
   const int head = (int)blockIdx.x % a.heads;
   const int q0 = (a.tiles - 1 - (int)blockIdx.x / a.heads) * 128;       // the rows with most keys first
   if (warp == 0) {
@@ -78,7 +80,11 @@ attention_window_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
         ptx::mbar_init(bar_v + 8 * i, 1);
       }
       ptx::mbar_init(bar_s, 1);
-      ptx::mbar_init(bar_pv, 1);
+      ptx::mbar_init(bar_free, 4);
+      for (int i = 0; i < 2; ++i) {
+        ptx::mbar_init(bar_p + 8 * i, 4);
+        ptx::mbar_init(bar_pv + 8 * i, 1);
+      }
       ptx::fence_mbar_init();
       ptx::tma_prefetch_desc(&map_q);
       ptx::tma_prefetch_desc(&map_kv);
@@ -93,7 +99,7 @@ attention_window_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
   // ---- this row's sequence: the last b with cu[b] <= row, searched 32-fold for the warp's first row, on from there
   const int row = min(q0 + r, a.T - 1);
   int lo_b = 0, hi_b = a.B;
-  const int row_w = min(q0 + (warp & 3) * 32, a.T - 1);
+  const int row_w = min(q0 + (warp & 3) * 32, a.T - 1);     // (the fifth warp repeats the first one's)
   while (hi_b - lo_b > 1) {
     const int step = (hi_b - lo_b + 31) / 32, i = lo_b + lane * step;
     const uint32_t le = __ballot_sync(0xffffffffu, i < hi_b && (lane == 0 || ptx::ld_dep(a.cu + i) <= row_w));
@@ -109,7 +115,7 @@ attention_window_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
   const bool real = q0 + r < a.T && row >= c0 && row < c1;
   const int first = real ? max(c0, 0) : row;                 // of the sequence; a row of none sees itself and is not stored
   const int low = max(first, row - (a.window > 0 ? a.window : a.max_len) + 1);
-  const bool bad = real && c1 - c0 > a.max_len;
+  const bool bad = real && tid < 128 && c1 - c0 > a.max_len;
   if (tid == 0) { s_bounds[0] = low; s_bounds[1] = first; }
   if (tid == 127) s_bounds[2] = low;       // (of the tile's last row)
   ptx::tc_fence_before_sync();
@@ -131,11 +137,12 @@ attention_window_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
     if (a.window > 0) m |= bits_between(first - j0, sinks_end - j0);
     return m;
   };
-  auto whole = [&](int i) { return i >= lead && base_of(i) >= low_last && base_of(i) + kKeys - 1 <= q0; };
+  // tiles whose keys every row sees: [whole0, whole1)
+  const int whole0 = lead + (low_last - key_w + kKeys - 1) / kKeys, whole1 = lead + (q0 + 1 >= key_w + kKeys ? (q0 + 1 - key_w) / kKeys : 0);
+  auto whole = [&](int i) { return i >= whole0 && i < whole1; };
 
   const int kvh = head / (a.heads / a.kv_heads);
   const int col_k = (a.heads + kvh) * kHeadDim, col_v = col_k + a.kv_heads * kHeadDim;
-  int k_loads = 0, v_loads = 0;                    // (warp 0) pairs of K tiles and V tiles requested
   auto load_k = [&](int s) {                       // pair s of pass A, then of pass B
     const int i = 2 * (s < np ? s : s - np);
     const uint32_t bar = bar_k + 8 * (s & 1), dst = ptx::smem_addr(sK) + (s & 1) * 2 * kSlot;
@@ -147,6 +154,9 @@ attention_window_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
     ptx::mbar_arrive_expect_tx(bar_v + 8 * (i & 1), kSlot);
     ptx::tma_load_2d(ptx::smem_addr(sV) + (i & 1) * kSlot, &map_kv, bar_v + 8 * (i & 1), col_v, base_of(i));
   };
+  auto wait = [](uint32_t bar, int use) {          // for the use-th completion of a barrier, by a whole warp
+    return __all_sync(0xffffffffu, ptx::mbar_wait(bar, (uint32_t)use & 1u)) != 0;
+  };
   const uint64_t dq = ptx::make_kmajor_desc(ptx::smem_addr(sQ), 512, ptx::kSwizzle64);
   auto score_mma = [&](uint32_t k_addr, int n) {   // S = Q K^T over n keys: 64 dimensions are two K steps
     const uint32_t idesc = ptx::make_idesc_i8(128, n, true, true);
@@ -157,198 +167,192 @@ attention_window_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
   };
 
   bool ok = true;
-  if (nt > 0 && warp == 0) {
+  if (nt > 0 && warp == 4) {
+    // ---- copies and matrix products.  Score tile u (pass A: pairs of tiles 0 .. np - 1, pass B: tiles np ..) may be issued when
+    // the four warps have read the one before; a pair of K tiles is replaced when its last scores have been read.
+    int k_loads = min(2, 2 * np), v_loads = min(2, nt);
     if (ptx::elect_one()) {
       ptx::mbar_arrive_expect_tx(bar_q, 128 * kHeadDim);
       ptx::tma_load_2d(ptx::smem_addr(sQ), &map_q, bar_q, head * kHeadDim, q0);
-      load_k(0);
-      load_k(1);
-      load_v(0);
-    }
-    k_loads = 2;
-    v_loads = 1;
-    ok = __all_sync(0xffffffffu, ptx::mbar_wait(bar_q, 0));
-  }
-
-  // ---- pass A: row maxima, 128 keys at a time
-  int32_t mx = INT32_MIN;
-  uint32_t s_phase = 0;
-  for (int p = 0; p < np; ++p) {
-    if (warp == 0) {
-      if (ok) ok = __all_sync(0xffffffffu, ptx::mbar_wait(bar_k + 8 * (p & 1), (p >> 1) & 1));
-      if (ok && ptx::elect_one()) {
-        ptx::tc_fence_after_sync();
-        score_mma(ptx::smem_addr(sK) + (p & 1) * 2 * kSlot, 2 * p + 1 < nt ? 128 : 64);
-      }
-      __syncwarp();
-    }
-    if (ok) ok = __all_sync(0xffffffffu, ptx::mbar_wait(bar_s, s_phase));
-    s_phase ^= 1;
-    if (warp == 0 && ok && p + 2 < 2 * np) {
-      if (ptx::elect_one()) load_k(p + 2);
-      __syncwarp();
-      k_loads = p + 3;
-    }
-    if (ok) {
-      ptx::tc_fence_after_sync();
-      const int i = 2 * p + half;                  // half of the threads takes each of the pair's tiles
-      if (i < nt) {
-        const uint64_t m = whole(i) ? ~0ull : mask_of(i);
-#pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          uint32_t v[32];
-          ptx::tmem_ld32(t_row + half * kKeys + c * 32, v);
-          ptx::tmem_wait_ld();
-          const uint32_t mc = (uint32_t)(m >> (32 * c));
-          if (__any_sync(0xffffffffu, mc != 0xffffffffu)) {
-#pragma unroll
-            for (int j = 0; j < 32; ++j)
-              if (!((mc >> j) & 1u)) v[j] = (uint32_t)INT32_MIN;
-          }
-#pragma unroll
-          for (int j = 0; j < 32; j += 2) mx = __vimax3_s32(mx, (int32_t)v[j], (int32_t)v[j + 1]);
-        }
-      }
-    }
-    ptx::tc_fence_before_sync();
-    ok = __syncthreads_and(ok);
-    if (!ok) break;
-  }
-
-  s_join[tid] = mx;
-  __syncthreads();
-  mx = max(s_join[r], s_join[128 + r]);
-
-  // ---- pass B: weights, O = sum w v
-  const LongAttnConsts& k = a.k;
-  const ExpConsts& ek = k.e;
-  const int64_t mk = iexp_folded_addend(ek);
-  const int32_t neg_m = -(int32_t)ek.fold_m, wk = iexp_folded_offset(ek, mx);
-  auto weight = [&](uint32_t s) {                  // w in the upper byte
-    uint32_t e;
-    if constexpr (MODE == 0) e = iexp_folded(add_alu((int32_t)s, wk, a.int_min), mk, neg_m, ek.q_ln2, ek.q_c);
-    else if constexpr (MODE == 1) e = iexp_folded((int32_t)(s + (uint32_t)wk) >> ek.s_in, mk, neg_m, ek.q_ln2, ek.q_c);
-    else e = iexp_dist_wide((uint32_t)mx - s, ek);
-    return e * k.b_w + (1u << 23);
-  };
-  uint32_t sum = 0;
-  if (nt > 0 && ok && warp == 0) {
-    ok = __all_sync(0xffffffffu, ptx::mbar_wait(bar_k + 8 * (np & 1), (np >> 1) & 1));
-    if (ok && ptx::elect_one()) {
-      ptx::tc_fence_after_sync();
-      score_mma(ptx::smem_addr(sK) + (np & 1) * 2 * kSlot, 64);
+      for (int s = 0; s < k_loads; ++s) load_k(s);
+      for (int i = 0; i < v_loads; ++i) load_v(i);
     }
     __syncwarp();
-  }
-  for (int i = 0; i < nt; ++i) {
-    uint32_t v[32];
-    if (ok) ok = __all_sync(0xffffffffu, ptx::mbar_wait(bar_s, s_phase));
-    s_phase ^= 1;
-    if (ok) {
-      ptx::tc_fence_after_sync();
-      ptx::tmem_ld32(t_row + 32 * half, v);
-      ptx::tmem_wait_ld();
-    }
-    ptx::tc_fence_before_sync();
-    ok = __syncthreads_and(ok);                    // every row's scores are in registers
-    if (!ok) break;
-    if (warp == 0) {
-      const int s = np + (i >> 1);                 // pair of tile i; a pair is done with its second (or the last) tile
-      if ((i & 1) && s + 2 < 2 * np) {
-        if (ptx::elect_one()) load_k(s + 2);
-        __syncwarp();
-        k_loads = s + 3;
+    ok = wait(bar_q, 0);
+    auto next_pair = [&]() {
+      if (k_loads >= 2 * np) return;
+      if (ptx::elect_one()) load_k(k_loads);
+      __syncwarp();
+      ++k_loads;
+    };
+    for (int u = 0; u < np && ok; ++u) {
+      if (u > 0) {
+        ok = wait(bar_free, u - 1);
+        if (!ok) break;
+        next_pair();
       }
-      if (i + 1 < nt) {
-        const int s1 = np + ((i + 1) >> 1);
-        if (!((i + 1) & 1)) ok = __all_sync(0xffffffffu, ptx::mbar_wait(bar_k + 8 * (s1 & 1), (s1 >> 1) & 1));
-        if (ok && ptx::elect_one()) {
+      ok = wait(bar_k + 8 * (u & 1), u >> 1);
+      if (!ok) break;
+      if (ptx::elect_one()) {
+        ptx::tc_fence_after_sync();
+        score_mma(ptx::smem_addr(sK) + (u & 1) * 2 * kSlot, 2 * u + 1 < nt ? 128 : 64);
+      }
+      __syncwarp();
+    }
+    for (int i = 0; i <= nt && ok; ++i) {
+      // scores of tile i, behind the reading of those before
+      if (i < nt) {
+        ok = wait(bar_free, np + i - 1);
+        if (!ok) break;
+        if (!(i & 1)) next_pair();
+        const int s = np + (i >> 1);
+        if (!(i & 1)) ok = wait(bar_k + 8 * (s & 1), s >> 1);
+        if (!ok) break;
+        if (ptx::elect_one()) {
           ptx::tc_fence_after_sync();
-          score_mma(ptx::smem_addr(sK) + (s1 & 1) * 2 * kSlot + ((i + 1) & 1) * kSlot, 64);
+          score_mma(ptx::smem_addr(sK) + (s & 1) * 2 * kSlot + (i & 1) * kSlot, 64);
         }
         __syncwarp();
       }
-    }
-    uint32_t w[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-      w[j] = __byte_perm(__byte_perm(weight(v[4 * j]), weight(v[4 * j + 1]), 0x0073),
-                         __byte_perm(weight(v[4 * j + 2]), weight(v[4 * j + 3]), 0x0073), 0x5410);
-    if (!whole(i)) {
-      const uint32_t m = (uint32_t)(mask_of(i) >> (32 * half));
-#pragma unroll
-      for (int j = 0; j < 8; ++j) w[j] &= byte_mask(m >> (4 * j));
-    }
-#pragma unroll
-    for (int j = 0; j < 8; ++j) sum = __dp4a(w[j], 0x01010101u, sum);
-    if (i > 0) {                                   // the product before has read P and its V
-      if (ok) ok = __all_sync(0xffffffffu, ptx::mbar_wait(bar_pv, (i - 1) & 1));
-    }
-    if (warp == 0 && ok && i + 1 < nt) {
-      if (ptx::elect_one()) load_v(i + 1);
-      __syncwarp();
-      v_loads = i + 2;
-    }
-#pragma unroll
-    for (int c = 0; c < 2; ++c)
-      *reinterpret_cast<uint4*>(sP + r * kKeys + (((2 * half + c) ^ ((r >> 1) & 3)) << 4)) =
-          make_uint4(w[4 * c], w[4 * c + 1], w[4 * c + 2], w[4 * c + 3]);
-    ptx::fence_proxy_async_smem();
-    if (warp == 0 && ok) ok = __all_sync(0xffffffffu, ptx::mbar_wait(bar_v + 8 * (i & 1), (i >> 1) & 1));
-    ptx::tc_fence_before_sync();
-    ok = __syncthreads_and(ok);                    // P complete
-    if (!ok) break;
-    if (warp == 0) {
+      if (i == 0) continue;
+      // O += P V of tile i - 1
+      const int p = i - 1;
+      ok = wait(bar_p + 8 * (p & 1), p >> 1);
+      if (ok) ok = wait(bar_v + 8 * (p & 1), p >> 1);
+      if (!ok) break;
       if (ptx::elect_one()) {
         ptx::tc_fence_after_sync();
         const uint32_t idesc = ptx::make_idesc_i8(128, kHeadDim, false, true) | (1u << 16);      // u8 x s8, V MN-major
-        const uint64_t dp = ptx::make_kmajor_desc(ptx::smem_addr(sP), 512, ptx::kSwizzle64);
+        const uint64_t dp = ptx::make_kmajor_desc(ptx::smem_addr(sP) + (p & 1) * kP, 512, ptx::kSwizzle64);
 #pragma unroll
         for (int kk = 0; kk < 2; ++kk) {
-          const uint32_t va = ptx::smem_addr(sV) + (i & 1) * kSlot + kk * 32 * kHeadDim;
+          const uint32_t va = ptx::smem_addr(sV) + (p & 1) * kSlot + kk * 32 * kHeadDim;
           const uint64_t dv = (uint64_t)((va & 0x3FFFFu) >> 4) | ((uint64_t)(512 >> 4) << 16) | ((uint64_t)(512 >> 4) << 32) |
                               ((uint64_t)1 << 46) | ((uint64_t)ptx::kSwizzle64 << 61);
-          ptx::mma_i8_ss(tmem + kKeys, dp + 2 * kk, dv, idesc, i + kk > 0 ? 1u : 0u);
+          ptx::mma_i8_ss(tmem + kKeys, dp + 2 * kk, dv, idesc, p + kk > 0 ? 1u : 0u);
         }
-        ptx::mma_commit(bar_pv);
+        ptx::mma_commit(bar_pv + 8 * (p & 1));
       }
       __syncwarp();
-    }
-  }
-  if (nt > 0 && ok) ok = __all_sync(0xffffffffu, ptx::mbar_wait(bar_pv, (nt - 1) & 1));
-
-  // ---- the weighted mean of this row, 32 dimensions per thread
-  __syncthreads();                                 // (the maxima have been read)
-  s_join[tid] = (int32_t)sum;
-  __syncthreads();
-  sum = (uint32_t)s_join[r] + (uint32_t)s_join[128 + r];
-  if (nt > 0 && ok) {
-    ptx::tc_fence_after_sync();
-    uint32_t v[32];
-    ptx::tmem_ld32(t_row + kKeys + 32 * half, v);
-    ptx::tmem_wait_ld();
-    if (real) {
-      const RowShare share = row_share(sum, k);
-      int8_t* o = a.out + ((int64_t)row * a.heads + head) * kHeadDim + 32 * half;
-#pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        uint32_t w[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-          w[j] = pack4_sat_s8(weighted_mean((int32_t)v[16 * c + 4 * j], share), weighted_mean((int32_t)v[16 * c + 4 * j + 1], share),
-                              weighted_mean((int32_t)v[16 * c + 4 * j + 2], share), weighted_mean((int32_t)v[16 * c + 4 * j + 3], share));
-        reinterpret_cast<uint4*>(o)[c] = make_uint4(w[0], w[1], w[2], w[3]);
+      if (p > 0 && p + 1 < nt) {                   // V of tile p - 1 has been read: the next one takes its place
+        ok = wait(bar_pv + 8 * ((p - 1) & 1), (p - 1) >> 1);
+        if (!ok) break;
+        if (ptx::elect_one()) load_v(p + 1);
+        __syncwarp();
+        ++v_loads;
       }
     }
-  }
-  if (!ok) {
-    atomicCAS(a.status, 0, IBERT_ERR_TIMEOUT);
-    if (warp == 0) {                               // copies still in flight land before the shared memory is given up
+    if (!ok) {                                     // copies still in flight land before the shared memory is given up
       for (int s = max(k_loads - 2, 0); s < k_loads; ++s) ptx::mbar_wait(bar_k + 8 * (s & 1), (s >> 1) & 1);
       for (int i = max(v_loads - 2, 0); i < v_loads; ++i) ptx::mbar_wait(bar_v + 8 * (i & 1), (i >> 1) & 1);
       ptx::mbar_wait(bar_q, 0);
     }
+  } else if (nt > 0) {
+    // ---- pass A: row maxima, 128 keys at a time
+    int32_t mx = INT32_MIN;
+    auto arrive = [&](uint32_t bar) {              // of this warp, after what its lanes did with tensor or shared memory
+      ptx::tc_fence_before_sync();
+      __syncwarp();
+      if (lane == 0) ptx::mbar_arrive(bar);
+    };
+    for (int u = 0; u < np; ++u) {
+      ok = wait(bar_s, u);
+      if (!ok) break;
+      ptx::tc_fence_after_sync();
+#pragma unroll 1
+      for (int h = 0; h < 2 && 2 * u + h < nt; ++h) {
+        uint32_t v[64];
+        ptx::tmem_ld64(t_row + h * kKeys, v);
+        ptx::tmem_wait_ld();
+        if (!whole(2 * u + h)) {
+          const uint64_t m = mask_of(2 * u + h);
+          const uint32_t m0 = (uint32_t)m, m1 = (uint32_t)(m >> 32);
+#pragma unroll
+          for (int j = 0; j < 64; ++j)
+            if (!(((j < 32 ? m0 : m1) >> (j & 31)) & 1u)) v[j] = (uint32_t)INT32_MIN;
+        }
+#pragma unroll
+        for (int j = 0; j < 64; j += 2) mx = __vimax3_s32(mx, (int32_t)v[j], (int32_t)v[j + 1]);
+      }
+      arrive(bar_free);
+    }
+
+    // ---- pass B: weights, O = sum w v
+    const LongAttnConsts& k = a.k;
+    const ExpConsts& ek = k.e;
+    const int64_t mk = iexp_folded_addend(ek);
+    const int32_t neg_m = -(int32_t)ek.fold_m, wk = iexp_folded_offset(ek, mx);
+    auto weight = [&](uint32_t s) {                // w in the upper byte
+      uint32_t e;
+      if constexpr (MODE == 0) e = iexp_folded(add_alu((int32_t)s, wk, a.int_min), mk, neg_m, ek.q_ln2, ek.q_c);
+      else if constexpr (MODE == 1) e = iexp_folded((int32_t)(s + (uint32_t)wk) >> ek.s_in, mk, neg_m, ek.q_ln2, ek.q_c);
+      else e = iexp_dist_wide((uint32_t)mx - s, ek);
+      return e * k.b_w + (1u << 23);
+    };
+    uint32_t sum = 0;
+    for (int i = 0; i < nt && ok; ++i) {
+      ok = wait(bar_s, np + i);
+      if (!ok) break;
+      ptx::tc_fence_after_sync();
+      const uint64_t m = whole(i) ? ~0ull : mask_of(i);
+      uint8_t* p_row = sP + (i & 1) * kP + r * kKeys;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        uint32_t v[32], w[8];
+        ptx::tmem_ld32(t_row + 32 * h, v);
+        ptx::tmem_wait_ld();
+        if (h == 1) arrive(bar_free);
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          w[j] = __byte_perm(__byte_perm(weight(v[4 * j]), weight(v[4 * j + 1]), 0x0073),
+                             __byte_perm(weight(v[4 * j + 2]), weight(v[4 * j + 3]), 0x0073), 0x5410);
+        const uint32_t mh = (uint32_t)(m >> (32 * h));
+        if (mh != 0xffffffffu) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) w[j] &= byte_mask(mh >> (4 * j));
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sum = __dp4a(w[j], 0x01010101u, sum);
+        if (h == 0 && i > 1) {                     // the product before the last has read this buffer
+          ok = wait(bar_pv + 8 * (i & 1), (i - 2) >> 1);
+          if (!ok) break;
+        }
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+          *reinterpret_cast<uint4*>(p_row + (((2 * h + c) ^ ((r >> 1) & 3)) << 4)) =
+              make_uint4(w[4 * c], w[4 * c + 1], w[4 * c + 2], w[4 * c + 3]);
+      }
+      if (!ok) break;
+      ptx::fence_proxy_async_smem();
+      arrive(bar_p + 8 * (i & 1));
+    }
+    if (ok) ok = wait(bar_pv + 8 * ((nt - 1) & 1), (nt - 1) >> 1);
+
+    // ---- the weighted mean of this row
+    if (ok) {
+      ptx::tc_fence_after_sync();
+      const RowShare share = row_share(sum, k);
+      int8_t* o = a.out + ((int64_t)row * a.heads + head) * kHeadDim;
+#pragma unroll 1
+      for (int h = 0; h < 2; ++h) {
+        uint32_t v[32];
+        ptx::tmem_ld32(t_row + kKeys + 32 * h, v);
+        ptx::tmem_wait_ld();
+        if (real) {
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+            uint32_t w[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              w[j] = pack4_sat_s8(weighted_mean((int32_t)v[16 * c + 4 * j], share), weighted_mean((int32_t)v[16 * c + 4 * j + 1], share),
+                                  weighted_mean((int32_t)v[16 * c + 4 * j + 2], share), weighted_mean((int32_t)v[16 * c + 4 * j + 3], share));
+            reinterpret_cast<uint4*>(o + 32 * h)[c] = make_uint4(w[0], w[1], w[2], w[3]);
+          }
+        }
+      }
+    }
   }
+  if (!ok) atomicCAS(a.status, 0, IBERT_ERR_TIMEOUT);
   if (bad) atomicCAS(a.status, 0, IBERT_ERR_VALUE_RANGE);
   ptx::tc_fence_before_sync();
   __syncthreads();
@@ -374,12 +378,16 @@ int launch_attention_window(ibert_ctx* ctx, const int8_t* qkv, const int32_t* cu
   a.tiles = (int32_t)((T + 127) / 128); a.int_min = INT32_MIN; a.k = k;
   const int64_t grid = (int64_t)a.tiles * heads;
   if (grid > INT32_MAX) return IBERT_ERR_SHAPE;
-  auto kernel = !iexp_takes_folded(k.e) ? attention_window_kernel<2>
-                : k.e.s_in == 0         ? attention_window_kernel<0>
-                                        : attention_window_kernel<1>;
-  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kWinSmem) != cudaSuccess) {
-    cudaGetLastError();
-    return IBERT_ERR_CUDA;
+  const int mode = !iexp_takes_folded(k.e) ? 2 : (k.e.s_in == 0 ? 0 : 1);
+  auto kernel = mode == 2 ? attention_window_kernel<2> : mode == 1 ? attention_window_kernel<1> : attention_window_kernel<0>;
+  static bool set[kMaxDevices][3] = {{false}};
+  bool& done = set[ctx->device % kMaxDevices][mode];
+  if (!done) {
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kWinSmem) != cudaSuccess) {
+      cudaGetLastError();
+      return IBERT_ERR_CUDA;
+    }
+    done = true;
   }
   return launch_pdl(kernel, dim3((unsigned)grid), dim3(kWinThreads), (size_t)kWinSmem, ctx->stream, 1, mq, mkv, a);
 }
