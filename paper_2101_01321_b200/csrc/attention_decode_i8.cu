@@ -77,7 +77,7 @@ __device__ __forceinline__ void transpose4(const uint32_t* w, uint32_t* o) {
 // the weights that it needs itself.  For one or two heads the eight weights per lane and tile would be those of an eighth or a
 // quarter of the lanes; for more, the scores' 4 bytes per head and key take the shared memory that the loads in flight need.
 template <int W, int STAGES, bool KEEP>
-__global__ void __launch_bounds__(32 * W, KEEP ? 5 : 3)
+__global__ void __launch_bounds__(32 * W, KEEP ? 5 : 4)
 attention_decode_kernel(const __grid_constant__ DecodeArgs a) {
   constexpr int kThreads = 32 * W;
   extern __shared__ __align__(16) uint8_t smem[];
@@ -114,12 +114,12 @@ attention_decode_kernel(const __grid_constant__ DecodeArgs a) {
   auto first_key = [&](int i) { return (i < lead ? i : i - lead + tile_w) * kTile; };
   auto seen = [&](int key) { return key < len && (key >= start || key < first); };
   // Byte offsets in either cache of keys 0 and 16 of every tile of this CTA.  A page holds whole halves of tiles, and rows of
-  // it past the sequence's end may be read as well as any.  Bit 0: some of the half's keys are not visible; bit 1: none is, or
-  // there is no such page (the offset is then page 0's, which may be read too: the scores are masked, the weights 0).
+  // it past the sequence's end may be read as well as any.  Bit 0: some of the half's keys are not visible; -1: none is, or
+  // there is no such page: nothing is copied, and whatever the ring holds gets masked scores and weights of 0.
   int64_t* s_place = reinterpret_cast<int64_t*>(s_score + (KEEP ? G * a.score_pitch : 0));
   for (int i = tid; i < 2 * (i1 - i0); i += kThreads) {
     const int key0 = first_key(i0 + (i >> 1)) + 16 * (i & 1);
-    int64_t place = 3;
+    int64_t place = -1;
     if (key0 < len && (key0 + 15 >= start || key0 < first)) {
       const int32_t page = ptx::ld_dep(a.tables + (int64_t)batch * a.max_pages + (key0 >> a.log_page));
       if ((uint32_t)page < (uint32_t)a.n_pages) {
@@ -146,12 +146,16 @@ attention_decode_kernel(const __grid_constant__ DecodeArgs a) {
       const bool keys = n < n_tiles || (!KEEP && !(m & 1));
       const longlong2 p = *reinterpret_cast<const longlong2*>(s_place + 2 * (warp + i * W));
       const int8_t* base = keys ? a.k_cache + k_lane : a.v_cache + v_lane;
-      const int8_t *lo = base + (p.x & ~int64_t(3)), *hi = base + (p.y & ~int64_t(3));
+      const int8_t *lo = base + (p.x & ~int64_t(1)), *hi = base + (p.y & ~int64_t(1));
       const uint32_t dst = ptx::smem_addr(ring + (n & (STAGES - 1)) * kTileBytes + lane * 16);
-      ptx::cp_async_16(dst, lo);
-      ptx::cp_async_16(dst + 512, lo + 512);
-      ptx::cp_async_16(dst + 1024, hi);
-      ptx::cp_async_16(dst + 1536, hi + 512);
+      if (p.x >= 0) {
+        ptx::cp_async_16(dst, lo);
+        ptx::cp_async_16(dst + 512, lo + 512);
+      }
+      if (p.y >= 0) {
+        ptx::cp_async_16(dst + 1024, hi);
+        ptx::cp_async_16(dst + 1536, hi + 512);
+      }
     }
     ptx::cp_async_commit();
   };
@@ -166,16 +170,17 @@ attention_decode_kernel(const __grid_constant__ DecodeArgs a) {
       mma_s8_first(c[j], q.x, 0u, q.y, 0u, r.x, r.y);
       mma_s8(c[j], q.z, 0u, q.w, 0u, r.z, r.w);
     }
-    const int2 flags = make_int2((int)s_place[2 * (warp + i * W)] & 3, (int)s_place[2 * (warp + i * W) + 1] & 3);
-    if (flags.x | flags.y) {
+    const int2 flags = make_int2((int)s_place[2 * (warp + i * W)], (int)s_place[2 * (warp + i * W) + 1]);
+    const bool masked = (flags.x | flags.y) & 1;              // (-1 has bit 0, too)
+    if (masked) {
       const int key0 = first_key(i0 + warp + i * W) + t;
 #pragma unroll
       for (int j = 0; j < 4; ++j)
 #pragma unroll
         for (int e = 0; e < 2; ++e)
-          if (((j < 2 ? flags.x : flags.y) & 2) || !seen(key0 + 8 * j + 4 * e)) c[j][e] = kNone;
+          if ((j < 2 ? flags.x : flags.y) == -1 || !seen(key0 + 8 * j + 4 * e)) c[j][e] = kNone;
     }
-    return (flags.x | flags.y) != 0;
+    return masked;
   };
 #pragma unroll
   for (int n = 0; n < STAGES; ++n) issue(n);
@@ -344,9 +349,7 @@ int launch_attention_decode(ibert_ctx* ctx, const int8_t* q, const int8_t* k_cac
   a.q = q; a.k_cache = k_cache; a.v_cache = v_cache; a.tables = tables; a.lens = lens; a.out = out; a.status = ctx->d_status;
   a.heads = heads; a.kv_heads = kv_heads; a.group = heads / kv_heads;
   a.tiles_of_group = (a.group + kMaxGroup - 1) / kMaxGroup;
-  a.log_page = log_page; a.max_pages = max_pages; a.n_pages = n_pages;
-  a.max_len = n_pages > 0 ? max_len : 0;               // (without pages there are no keys)
-  a.window = window; a.sinks = sinks;
+  a.log_page = log_page; a.max_pages = max_pages; a.n_pages = n_pages; a.max_len = max_len; a.window = window; a.sinks = sinks;
   a.k = k;
   const int64_t items = (int64_t)B * kv_heads * a.tiles_of_group;
   // tiles of 32 keys that a sequence can have: one more where the window starts inside a tile, and the sinks' own
