@@ -16,8 +16,8 @@
 // The products run on mma.sync m16n8k32 (s8 x s8, s8 x u8): up to eight query heads of a group, and the kernel is bound by
 // the 128 bytes per key and the instructions around them, not by the tensor pipe.  S^T = Q K^T leaves a lane with one head
 // and the very keys whose weights it needs as the B operand of O^T = V^T w; the 16 bytes of a key that a lane copies are
-// the operand of both K steps as they come (any order of the 64 dimensions will do if Q has the same); the values of four
-// keys are transposed in registers by byte permutes.
+// the operand of both K steps as they come (any order of the 64 dimensions will do if Q has the same); the values are
+// transposed on their way out of shared memory (ldmatrix of bytes), four keys to a register.
 #include <algorithm>
 
 #include "device_utils.cuh"
@@ -62,16 +62,6 @@ __device__ __forceinline__ void mma_s8u8(int32_t (&c)[4], uint32_t a0, uint32_t 
                : "+r"(c[0]), "+r"(c[1]), "+r"(c[2]), "+r"(c[3])
                : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-// bytes of four words, transposed: o[i] = byte i of w[0], w[1], w[2], w[3]
-__device__ __forceinline__ void transpose4(const uint32_t* w, uint32_t* o) {
-  const uint32_t a = __byte_perm(w[0], w[1], 0x5140), b = __byte_perm(w[0], w[1], 0x7362);
-  const uint32_t c = __byte_perm(w[2], w[3], 0x5140), d = __byte_perm(w[2], w[3], 0x7362);
-  o[0] = __byte_perm(a, c, 0x5410);
-  o[1] = __byte_perm(a, c, 0x7632);
-  o[2] = __byte_perm(b, d, 0x5410);
-  o[3] = __byte_perm(b, d, 0x7632);
-}
-
 // W warps with STAGES tiles of each in flight.  KEEP: the scores stay in shared memory from the maximum to the weights, and the
 // exponentials of a head are spread over all threads; else the keys are read a second time (out of L2) and every lane computes
 // the weights that it needs itself.  For one or two heads the eight weights per lane and tile would be those of an eighth or a
@@ -84,7 +74,7 @@ attention_decode_kernel(const __grid_constant__ DecodeArgs a) {
   int32_t* s_score = reinterpret_cast<int32_t*>(smem + W * STAGES * kTileBytes);               // KEEP: [heads][score_pitch]
   __shared__ int32_t s_all_max[kMaxCluster][kMaxGroup];       // by CTA of the cluster
   __shared__ int32_t s_warp_max[W][kMaxGroup];
-  __shared__ int32_t s_out[16][32];      // partial O: [4 i + c][lane] holds head 2 t + (c & 1), dimension 8 g + 2 i + (c >> 1)
+  __shared__ int32_t s_out[16][32];      // partial O: [4 i + c][lane] holds head 2 t + (c & 1), dimension 16 i + 8 (c >> 1) + g
   __shared__ int32_t s_sum[kMaxGroup];                        // partial W
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
@@ -137,9 +127,11 @@ attention_decode_kernel(const __grid_constant__ DecodeArgs a) {
   // keys and its values in turn.  The first of the second part are on their way while the CTAs meet.
   uint8_t* ring = smem + warp * STAGES * kTileBytes;
   const int n_tiles = i0 + warp < i1 ? (i1 - i0 - warp + W - 1) / W : 0, n_stream = (KEEP ? 2 : 3) * n_tiles;
-  // In a tile of keys, row n of eight is key (n & 1) 4 + (n >> 1): the two keys of a score fragment's lane t are then t and
-  // 4 + t, and the four lanes of a head read the values of four consecutive keys
-  const int k_lane = (((g & 1) << 2) + (g >> 1)) * kHeadDim + t * 16, v_lane = lane * 16;
+  // In a tile of keys, row n of the j-th eight is key 16 (j / 2) + 2 (j & 1) + 4 (n / 2) + (n & 1): a lane's two scores of the
+  // eights 2 p and 2 p + 1 are then those of keys 16 p + 4 t .. + 3, the four that a register of transposed values holds.  A
+  // tile of values lies in the ring with its 16-byte chunks swizzled: eight rows of a chunk are eight different bank groups.
+  const int k_lane = (((g >> 1) << 2) + (g & 1)) * kHeadDim + t * 16, v_lane = lane * 16;
+  const uint32_t k_dst = lane * 16, v_dst = g * kHeadDim + ((t ^ ((g >> 1) & 3)) << 4);
   auto issue = [&](int n) {              // tile n of the stream; a lane copies 16 bytes of each of its eight rows
     if (n < n_stream) {
       const int m = n - n_tiles, i = n < n_tiles ? n : (KEEP ? m : m >> 1);
@@ -147,20 +139,21 @@ attention_decode_kernel(const __grid_constant__ DecodeArgs a) {
       const longlong2 p = *reinterpret_cast<const longlong2*>(s_place + 2 * (warp + i * W));
       const int8_t* base = keys ? a.k_cache + k_lane : a.v_cache + v_lane;
       const int8_t *lo = base + (p.x & ~int64_t(1)), *hi = base + (p.y & ~int64_t(1));
-      const uint32_t dst = ptx::smem_addr(ring + (n & (STAGES - 1)) * kTileBytes + lane * 16);
+      const uint32_t dst = ptx::smem_addr(ring + (n & (STAGES - 1)) * kTileBytes) + (keys ? k_dst : v_dst);
+      const int second = keys ? 2 * kHeadDim : 8 * kHeadDim;             // from one eight rows of a half to the other
       if (p.x >= 0) {
         ptx::cp_async_16(dst, lo);
-        ptx::cp_async_16(dst + 512, lo + 512);
+        ptx::cp_async_16(dst + 512, lo + second);
       }
       if (p.y >= 0) {
         ptx::cp_async_16(dst + 1024, hi);
-        ptx::cp_async_16(dst + 1536, hi + 512);
+        ptx::cp_async_16(dst + 1536, hi + second);
       }
     }
     ptx::cp_async_commit();
   };
   constexpr int32_t kNone = INT32_MIN;
-  // scores of head g against keys 8 j + t and 8 j + 4 + t (c[j][0], c[j][1]) of a tile of keys that this lane copied itself,
+  // scores c[j][e] of head g against keys 16 (j / 2) + 4 t + 2 (j & 1) + e of a tile of keys that this lane copied itself,
   // and whether some of them are masked
   auto scores = [&](int n, int i, int32_t (&c)[4][4]) {
     const uint8_t* tile = ring + (n & (STAGES - 1)) * kTileBytes + lane * 16;
@@ -173,12 +166,12 @@ attention_decode_kernel(const __grid_constant__ DecodeArgs a) {
     const int2 flags = make_int2((int)s_place[2 * (warp + i * W)], (int)s_place[2 * (warp + i * W) + 1]);
     const bool masked = (flags.x | flags.y) & 1;              // (-1 has bit 0, too)
     if (masked) {
-      const int key0 = first_key(i0 + warp + i * W) + t;
+      const int key0 = first_key(i0 + warp + i * W) + 4 * t;
 #pragma unroll
       for (int j = 0; j < 4; ++j)
 #pragma unroll
         for (int e = 0; e < 2; ++e)
-          if ((j < 2 ? flags.x : flags.y) == -1 || !seen(key0 + 8 * j + 4 * e)) c[j][e] = kNone;
+          if ((j < 2 ? flags.x : flags.y) == -1 || !seen(key0 + 16 * (j >> 1) + 2 * (j & 1) + e)) c[j][e] = kNone;
     }
     return masked;
   };
@@ -194,7 +187,7 @@ attention_decode_kernel(const __grid_constant__ DecodeArgs a) {
     issue(n + STAGES);
 #pragma unroll
     for (int j = 0; j < 4; ++j) mx = __vimax3_s32(mx, c[j][0], c[j][1]);
-    if (KEEP && g < G) {                 // four to a later word: keys t, 4 + t, 8 + t, 12 + t and 16 + ..
+    if (KEEP && g < G) {                 // (in the order of the keys)
       int32_t* s_tile = s_score + g * a.score_pitch + (warp + n * W) * kTile + 4 * t;
 #pragma unroll
       for (int j = 0; j < 4; ++j)
@@ -215,26 +208,16 @@ attention_decode_kernel(const __grid_constant__ DecodeArgs a) {
 
   // ---- weights and O = sum w v
   const LongAttnConsts& k = a.k;
-  int32_t acc[4][4] = {};                                     // dims 8g + 2i (+ 1) x heads 2t, 2t + 1
-  auto accumulate = [&](int n, uint32_t w0, uint32_t w1) {    // a tile of values: rows t, 4 + t, .. 28 + t, 8 bytes of each
-    const uint8_t* tile = ring + (n & (STAGES - 1)) * kTileBytes + t * kHeadDim + g * 8;
-    uint32_t x[8], y[8], xt[8], yt[8];
+  int32_t acc[4][4] = {};                                     // dims 16 i + g (c < 2) and 16 i + 8 + g x heads 2t, 2t + 1
+  auto accumulate = [&](int n, uint32_t w0, uint32_t w1) {    // a tile of values; lane l addresses row l
+    const uint32_t row = ptx::smem_addr(ring + (n & (STAGES - 1)) * kTileBytes) + lane * kHeadDim;
+    uint32_t v[4][4];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const uint2 v = *reinterpret_cast<const uint2*>(tile + j * 4 * kHeadDim);
-      x[j] = v.x;
-      y[j] = v.y;
-    }
+    for (int i = 0; i < 4; ++i) ptx::ldmatrix_b8_t(v[i], row + ((i ^ ((lane >> 1) & 3)) << 4));
     __syncwarp();                        // every lane has read the tile
     issue(n + STAGES);
-    transpose4(x, xt);
-    transpose4(x + 4, xt + 4);
-    transpose4(y, yt);
-    transpose4(y + 4, yt + 4);
-    mma_s8u8(acc[0], xt[0], xt[1], xt[4], xt[5], w0, w1);
-    mma_s8u8(acc[1], xt[2], xt[3], xt[6], xt[7], w0, w1);
-    mma_s8u8(acc[2], yt[0], yt[1], yt[4], yt[5], w0, w1);
-    mma_s8u8(acc[3], yt[2], yt[3], yt[6], yt[7], w0, w1);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) mma_s8u8(acc[i], v[i][0], v[i][1], v[i][2], v[i][3], w0, w1);
   };
   auto pack = [](const uint32_t* e) {    // the upper bytes of four words
     return __byte_perm(__byte_perm(e[0], e[1], 0x0073), __byte_perm(e[2], e[3], 0x0073), 0x5410);
@@ -326,7 +309,7 @@ attention_decode_kernel(const __grid_constant__ DecodeArgs a) {
   // ---- every CTA joins and divides its part of the G x 64 results
   for (int i = (int)rank * kThreads + tid; i < G * kHeadDim; i += cl * kThreads) {
     const int h = i / kHeadDim, d = i % kHeadDim;
-    const int32_t* part = &s_out[((d & 7) >> 1) * 4 + ((d & 1) << 1) + (h & 1)][(d >> 3) * 4 + (h >> 1)];
+    const int32_t* part = &s_out[(d >> 4) * 4 + ((d >> 3) & 1) * 2 + (h & 1)][(d & 7) * 4 + (h >> 1)];
     int32_t o = 0;
     uint32_t total = 0;
     for (int c = 0; c < cl; ++c) {

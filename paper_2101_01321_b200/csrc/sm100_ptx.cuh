@@ -161,6 +161,14 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* m, 
       : "memory");
 }
 
+// Two 16 x 16 blocks of bytes, transposed: lanes 0 .. 15 address the 16-byte rows of the first, 16 .. 31 those of the second;
+// lane 4 g + t gets columns g (r[0]; second block r[2]) and g + 8 (r[1], r[3]), bytes of rows 4 t .. 4 t + 3
+__device__ __forceinline__ void ldmatrix_b8_t(uint32_t (&r)[4], uint32_t row) {
+  asm volatile("ldmatrix.sync.aligned.m16n16.x2.trans.shared.b8 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(row)
+               : "memory");
+}
 // 16 bytes global -> shared by the issuing thread's own asynchronous copy
 __device__ __forceinline__ void cp_async_16(uint32_t dst, const void* src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
