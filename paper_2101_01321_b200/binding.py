@@ -6,6 +6,7 @@ CPU path: if the library is missing or a call fails, an exception is raised.
 from __future__ import annotations
 
 import ctypes as C
+import struct
 from pathlib import Path
 
 import numpy as np
@@ -112,7 +113,7 @@ def lib():
         L.ibert_kv_slots.argtypes = [vp, vp, vp, vp, i32, i32, i32, vp, i64, vp, i64, vp, vp, vp, vp, vp]
         L.ibert_rope_frequencies.argtypes = [i32, dbl, dbl, dbl, dbl, dbl, vp]
         L.ibert_rope_rows.argtypes = [vp, i32, i64, i64, dbl, vp]
-        L.ibert_qkv_rope_i8.argtypes = [vp, C.POINTER(RopeDesc), vp, i64, vp, i32, vp, vp, vp, vp, vp]
+        L.ibert_qkv_rope_i8.argtypes = [vp, vp, vp, i64, vp, i32, vp, vp, vp, vp, vp]
         L.ibert_attention_decode_i8.argtypes = [vp, vp, vp, vp, vp, vp, i32, i32, i32, i64, i32, i32, i32, i32, i32, dbl, dbl, dbl,
                                                 dbl, i32, vp, vp]
         L.ibert_attention_window_i8.argtypes = [vp, vp, vp, i32, i32, i64, i32, i32, i32, i32, dbl, dbl, dbl, dbl, i32, vp, vp]
@@ -138,12 +139,20 @@ def _chk(rc: int, where: str):
 def _dev(t: torch.Tensor | None, dtype) -> int | None:
     if t is None:
         return None
-    assert t.is_cuda and t.is_contiguous() and t.dtype == dtype, (t.device, t.dtype, dtype)
+    assert t.is_cuda and t.is_contiguous() and t.dtype is dtype, (t.device, t.dtype, dtype)
     return t.data_ptr()
 
 
 def _host(a, dtype) -> np.ndarray:
     return np.ascontiguousarray(a, dtype=dtype)
+
+
+def _np_ptr(a: np.ndarray | None) -> int:
+    return 0 if a is None else a.__array_interface__["data"][0]
+
+
+_ROPE_DESC = struct.Struct("6i2q3P4d")        # RopeDesc, packed at once (field by field it takes as long as the call)
+assert _ROPE_DESC.size == C.sizeof(RopeDesc)
 
 
 def ibert_dyadic_from_double(m: float) -> tuple[int, int]:
@@ -521,32 +530,29 @@ class Context:
         page_size, 64].  Returns (out, (S_q, S_k, S_v))."""
         n = (heads + 2 * kv_heads) * 64
         T = qkv.numel() // n
-        assert qkv.numel() == T * n and qkv.dtype in (torch.int8, torch.int16)
-        d = RopeDesc(heads, kv_heads, 8 * qkv.element_size(), 0, int(interleaved), 0, 0, 0, None, None, None, S_in, S_q, S_k, S_v)
-        if gamma_q is not None:
-            gq = _host(gamma_q, np.float64)
-            assert gq.size == 64
-            d.gamma_q = gq.ctypes.data
-        if gamma_k is not None:
-            gk = _host(gamma_k, np.float64)
-            assert gk.size == 64
-            d.gamma_k = gk.ctypes.data
+        dtype = qkv.dtype
+        assert qkv.numel() == T * n and (dtype is torch.int8 or dtype is torch.int16)
+        gq = None if gamma_q is None else _host(gamma_q, np.float64)
+        gk = None if gamma_k is None else _host(gamma_k, np.float64)
+        assert (gq is None or gq.size == 64) and (gk is None or gk.size == 64)
+        max_pos = rot_dim = n_pages = page_size = 0
         if rope is not None:
-            d.max_pos, d.rot_dim = rope.shape
-            d.rope = _dev(rope, torch.int16)
+            max_pos, rot_dim = rope.shape
             assert positions is not None and positions.numel() == T
         if k_cache is not None:
-            assert k_cache.dim() == 4 and k_cache.shape[1] == kv_heads and k_cache.shape[3] == 64
-            assert v_cache is not None and v_cache.shape == k_cache.shape and slots is not None and slots.numel() == T
-            d.n_pages, _, d.page_size, _ = k_cache.shape
+            n_pages, h, page_size, D = k_cache.shape
+            assert h == kv_heads and D == 64 and v_cache is not None and v_cache.shape == k_cache.shape
+            assert slots is not None and slots.numel() == T
+        cols = n if with_kv else heads * 64
         if out is None:
-            out = torch.empty((T, n if with_kv else heads * 64), dtype=torch.int8, device=qkv.device)
-        assert out.numel() == T * (n if with_kv else heads * 64)
-        S_ret = (C.c_double * 3)()
-        _chk(lib().ibert_qkv_rope_i8(self.h, C.byref(d), _dev(qkv, qkv.dtype), T, _dev(positions, torch.int32), int(with_kv),
-                                     _dev(out, torch.int8), _dev(slots, torch.int32), _dev(k_cache, torch.int8),
-                                     _dev(v_cache, torch.int8), S_ret), "ibert_qkv_rope_i8")
-        return out, tuple(S_ret)
+            out = torch.empty((T, cols), dtype=torch.int8, device=qkv.device)
+        assert out.numel() == T * cols
+        desc = _ROPE_DESC.pack(heads, kv_heads, 8 if dtype is torch.int8 else 16, rot_dim, int(interleaved), page_size, n_pages, max_pos,
+                               _dev(rope, torch.int16) or 0, _np_ptr(gq), _np_ptr(gk), S_in, S_q, S_k, S_v)
+        i32, i8 = torch.int32, torch.int8
+        _chk(lib().ibert_qkv_rope_i8(self.h, desc, _dev(qkv, dtype), T, _dev(positions, i32), int(with_kv), _dev(out, i8),
+                                     _dev(slots, i32), _dev(k_cache, i8), _dev(v_cache, i8), None), "ibert_qkv_rope_i8")
+        return out, (S_q, S_k, S_v)
 
     def ibert_attention_window_i8(self, qkv: torch.Tensor, cu_seqlens: torch.Tensor, max_len: int, heads: int, kv_heads: int,
                                   S_q: float, S_k: float, S_v: float, S_ctx: float, window: int = 0, sinks: int = 0,
@@ -558,11 +564,10 @@ class Context:
         if out is None:
             out = qkv.new_empty((T, heads * 64))
         assert out.numel() == T * heads * 64
-        S_ret = C.c_double()
         _chk(lib().ibert_attention_window_i8(self.h, _dev(qkv, torch.int8), _dev(cu_seqlens, torch.int32), cu_seqlens.numel() - 1,
                                              max_len, T, heads, kv_heads, window, sinks, S_q, S_k, S_v, S_ctx, p_max,
-                                             _dev(out, torch.int8), C.byref(S_ret)), "ibert_attention_window_i8")
-        return out, S_ret.value
+                                             _dev(out, torch.int8), None), "ibert_attention_window_i8")
+        return out, S_ctx
 
     def ibert_attention_decode_i8(self, q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, block_tables: torch.Tensor,
                                   lens: torch.Tensor, max_len: int, heads: int, S_q: float, S_k: float, S_v: float, S_ctx: float,
@@ -575,12 +580,11 @@ class Context:
         if out is None:
             out = q.new_empty((B, heads * 64))
         assert out.numel() == q.numel()
-        S_ret = C.c_double()
         _chk(lib().ibert_attention_decode_i8(self.h, _dev(q, torch.int8), _dev(k_cache, torch.int8), _dev(v_cache, torch.int8),
                                              _dev(block_tables, torch.int32), _dev(lens, torch.int32), B, max_len, max_pages, n_pages,
                                              page_size, heads, kv_heads, window, sinks, S_q, S_k, S_v, S_ctx, p_max,
-                                             _dev(out, torch.int8), C.byref(S_ret)), "ibert_attention_decode_i8")
-        return out, S_ret.value
+                                             _dev(out, torch.int8), None), "ibert_attention_decode_i8")
+        return out, S_ctx
 
     # ------------------------------------------------------------------ encoder layer
     def ibert_layer_create(self, params: dict) -> "Layer":
