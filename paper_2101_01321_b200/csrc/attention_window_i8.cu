@@ -26,11 +26,11 @@
 namespace ibert {
 namespace {
 
-constexpr int kWinThreads = 160;                   // four warps of rows, one that feeds the tensor pipe
 constexpr int kKeys = 64;                          // keys per tile
 constexpr int kSlot = kKeys * kHeadDim;            // 4 KB
+constexpr int kVRing = 3;                          // V tiles in shared memory
 constexpr int kP = 128 * kKeys;                    // weights of a tile: 8 KB
-constexpr int kWinSmem = 128 * kHeadDim + 4 * kSlot + 2 * kSlot + 2 * kP + 256 + 1024;
+constexpr int kWinSmem = 128 * kHeadDim + 4 * kSlot + kVRing * kSlot + 2 * kP + 256 + 2 * 128 * 4 + 1024;
 
 struct WindowArgs {
   const int32_t* cu;                               // [B + 1]
@@ -52,21 +52,25 @@ __device__ __forceinline__ uint64_t bits_between(int a, int b) {
 __device__ __forceinline__ uint32_t byte_mask(uint32_t m) { return ((m & 15u) * 0x00204081u & 0x01010101u) * 255u; }
 
 // MODE: how i-exp is evaluated; 0: folded without a pre-shift, 1: folded with one, 2: the wide form
-template <int MODE>
-__global__ void __launch_bounds__(kWinThreads, 4)
+// SPLIT: threads per row, each with half of a tile's columns: while the CTAs are few, their rows' exponentials are the longest
+// part of every step (4 prompts of up to 97 tokens, 12 heads, 36 CTAs: NUM1 us by one thread, NUM2 by two)
+template <int MODE, int SPLIT>
+__global__ void __launch_bounds__(128 * SPLIT + 32, SPLIT == 1 ? 4 : 2)
 attention_window_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_kv,
                         const __grid_constant__ WindowArgs a) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint8_t* sQ = smem;                              // [128][64 B], 64-byte swizzle
   uint8_t* sK = sQ + 128 * kHeadDim;               // two pairs of tiles [64][64 B], 64-byte swizzle
-  uint8_t* sV = sK + 4 * kSlot;                    // two tiles
-  uint8_t* sP = sV + 2 * kSlot;                    // two of [128][64 B], 64-byte swizzle
+  uint8_t* sV = sK + 4 * kSlot;                    // kVRing tiles
+  uint8_t* sP = sV + kVRing * kSlot;                    // two of [128][64 B], 64-byte swizzle
   uint64_t* s_bar = reinterpret_cast<uint64_t*>(sP + 2 * kP);
   const uint32_t bar_q = ptx::smem_addr(s_bar), bar_k = bar_q + 8, bar_v = bar_q + 24;       // copies: Q, pairs of K tiles, V tiles
-  const uint32_t bar_s = bar_q + 40, bar_free = bar_q + 48;          // scores complete; scores read by the four warps
-  const uint32_t bar_p = bar_q + 56, bar_pv = bar_q + 72;            // weights written (two buffers); their product done
+  const uint32_t bar_s = bar_q + 48, bar_free = bar_q + 56;          // scores complete; scores read by the warps of the rows
+  const uint32_t bar_p = bar_q + 64, bar_pv = bar_q + 80;            // weights written (two buffers); the last product done
   uint32_t* s_tmem = reinterpret_cast<uint32_t*>(s_bar + 11);
+  constexpr int kRowWarps = 4 * SPLIT;
+  int32_t* s_join = reinterpret_cast<int32_t*>(s_bar + 32);    // [2][128] what the two threads of a row exchange
   int32_t* s_bounds = reinterpret_cast<int32_t*>(s_bar + 12);  // first visible key, first row of the sequence, last row's first key
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, r = tid & 127;
@@ -75,16 +79,12 @@ attention_window_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
   if (warp == 0) {
     if (ptx::elect_one()) {
       ptx::mbar_init(bar_q, 1);
-      for (int i = 0; i < 2; ++i) {
-        ptx::mbar_init(bar_k + 8 * i, 1);
-        ptx::mbar_init(bar_v + 8 * i, 1);
-      }
+      for (int i = 0; i < 2; ++i) ptx::mbar_init(bar_k + 8 * i, 1);
+      for (int i = 0; i < kVRing; ++i) ptx::mbar_init(bar_v + 8 * i, 1);
       ptx::mbar_init(bar_s, 1);
-      ptx::mbar_init(bar_free, 4);
-      for (int i = 0; i < 2; ++i) {
-        ptx::mbar_init(bar_p + 8 * i, 4);
-        ptx::mbar_init(bar_pv + 8 * i, 1);
-      }
+      ptx::mbar_init(bar_free, kRowWarps);
+      for (int i = 0; i < 2; ++i) ptx::mbar_init(bar_p + 8 * i, kRowWarps);
+      ptx::mbar_init(bar_pv, 1);
       ptx::fence_mbar_init();
       ptx::tma_prefetch_desc(&map_q);
       ptx::tma_prefetch_desc(&map_kv);
@@ -99,7 +99,7 @@ attention_window_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
   // ---- this row's sequence: the last b with cu[b] <= row, searched 32-fold for the warp's first row, on from there
   const int row = min(q0 + r, a.T - 1);
   int lo_b = 0, hi_b = a.B;
-  const int row_w = min(q0 + (warp & 3) * 32, a.T - 1);     // (the fifth warp repeats the first one's)
+  const int row_w = min(q0 + (warp & 3) * 32, a.T - 1);     // (the last warp repeats the first one's)
   while (hi_b - lo_b > 1) {
     const int step = (hi_b - lo_b + 31) / 32, i = lo_b + lane * step;
     const uint32_t le = __ballot_sync(0xffffffffu, i < hi_b && (lane == 0 || ptx::ld_dep(a.cu + i) <= row_w));
@@ -151,8 +151,9 @@ attention_window_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
     if (i + 1 < nt) ptx::tma_load_2d(dst + kSlot, &map_kv, bar, col_k, base_of(i + 1));
   };
   auto load_v = [&](int i) {
-    ptx::mbar_arrive_expect_tx(bar_v + 8 * (i & 1), kSlot);
-    ptx::tma_load_2d(ptx::smem_addr(sV) + (i & 1) * kSlot, &map_kv, bar_v + 8 * (i & 1), col_v, base_of(i));
+    const int at = i % kVRing;
+    ptx::mbar_arrive_expect_tx(bar_v + 8 * at, kSlot);
+    ptx::tma_load_2d(ptx::smem_addr(sV) + at * kSlot, &map_kv, bar_v + 8 * at, col_v, base_of(i));
   };
   auto wait = [](uint32_t bar, int use) {          // for the use-th completion of a barrier, by a whole warp
     return __all_sync(0xffffffffu, ptx::mbar_wait(bar, (uint32_t)use & 1u)) != 0;
@@ -167,89 +168,72 @@ attention_window_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
   };
 
   bool ok = true;
-  if (nt > 0 && warp == 4) {
-    // ---- copies and matrix products.  Score tile u (pass A: pairs of tiles 0 .. np - 1, pass B: tiles np ..) may be issued when
-    // the four warps have read the one before; a pair of K tiles is replaced when its last scores have been read.
-    int k_loads = min(2, 2 * np), v_loads = min(2, nt);
+  if (nt > 0 && warp == kRowWarps) {
+    // ---- copies and matrix products, all by one thread.  Score tile u (pass A: pairs of tiles 0 .. np - 1, pass B: tiles np ..)
+    // may be issued when the rows have read the one before; a pair of K tiles is replaced when its last scores have been read.
+    // Products complete in the order of their issue, and their barrier counts all that were issued before: scores that have
+    // been read say that the product of weights issued before them has read its weights and values, too.  (The values need
+    // three tiles, the weights two, for that; waits of their own for either cost this thread more than a step takes.)
     if (ptx::elect_one()) {
+      int k_loads = min(2, 2 * np), v_loads = min(kVRing, nt);
       ptx::mbar_arrive_expect_tx(bar_q, 128 * kHeadDim);
       ptx::tma_load_2d(ptx::smem_addr(sQ), &map_q, bar_q, head * kHeadDim, q0);
       for (int s = 0; s < k_loads; ++s) load_k(s);
       for (int i = 0; i < v_loads; ++i) load_v(i);
-    }
-    __syncwarp();
-    ok = wait(bar_q, 0);
-    auto next_pair = [&]() {
-      if (k_loads >= 2 * np) return;
-      if (ptx::elect_one()) load_k(k_loads);
-      __syncwarp();
-      ++k_loads;
-    };
-    for (int u = 0; u < np && ok; ++u) {
-      if (u > 0) {
-        ok = wait(bar_free, u - 1);
-        if (!ok) break;
-        next_pair();
-      }
-      ok = wait(bar_k + 8 * (u & 1), u >> 1);
-      if (!ok) break;
-      if (ptx::elect_one()) {
+      ok = ptx::mbar_wait(bar_q, 0);
+      for (int u = 0; u < np && ok; ++u) {
+        if (u > 0) {
+          if (!(ok = ptx::mbar_wait(bar_free, (u - 1) & 1))) break;
+          if (k_loads < 2 * np) load_k(k_loads++);
+        }
+        if (!(ok = ptx::mbar_wait(bar_k + 8 * (u & 1), (u >> 1) & 1))) break;
         ptx::tc_fence_after_sync();
         score_mma(ptx::smem_addr(sK) + (u & 1) * 2 * kSlot, 2 * u + 1 < nt ? 128 : 64);
       }
-      __syncwarp();
-    }
-    for (int i = 0; i <= nt && ok; ++i) {
-      // scores of tile i, behind the reading of those before
-      if (i < nt) {
-        ok = wait(bar_free, np + i - 1);
-        if (!ok) break;
-        if (!(i & 1)) next_pair();
-        const int s = np + (i >> 1);
-        if (!(i & 1)) ok = wait(bar_k + 8 * (s & 1), s >> 1);
-        if (!ok) break;
-        if (ptx::elect_one()) {
+      const uint32_t idesc = ptx::make_idesc_i8(128, kHeadDim, false, true) | (1u << 16);        // u8 x s8, V MN-major
+      const uint64_t dp = ptx::make_kmajor_desc(ptx::smem_addr(sP), 512, ptx::kSwizzle64);
+      const uint64_t dv = (uint64_t)((ptx::smem_addr(sV) & 0x3FFFFu) >> 4) | ((uint64_t)(512 >> 4) << 16) |
+                          ((uint64_t)(512 >> 4) << 32) | ((uint64_t)1 << 46) | ((uint64_t)ptx::kSwizzle64 << 61);
+      int v_at = 0, v_phase = 0;                   // of tile i - 1
+      for (int i = 0; i <= nt && ok; ++i) {
+        if (i < nt) {                              // scores of tile i
+          const int s = np + (i >> 1);
+          if (!(ok = ptx::mbar_wait(bar_free, (np + i - 1) & 1))) break;
+          if (!(i & 1) && !(ok = ptx::mbar_wait(bar_k + 8 * (s & 1), (s >> 1) & 1))) break;
           ptx::tc_fence_after_sync();
           score_mma(ptx::smem_addr(sK) + (s & 1) * 2 * kSlot + (i & 1) * kSlot, 64);
+          if (!(i & 1) && k_loads < 2 * np) load_k(k_loads++);
+          if (i >= kVRing) { load_v(i); ++v_loads; }
         }
-        __syncwarp();
-      }
-      if (i == 0) continue;
-      // O += P V of tile i - 1
-      const int p = i - 1;
-      ok = wait(bar_p + 8 * (p & 1), p >> 1);
-      if (ok) ok = wait(bar_v + 8 * (p & 1), p >> 1);
-      if (!ok) break;
-      if (ptx::elect_one()) {
+        if (i == 0) continue;
+        const int p = i - 1;                       // O += P V of tile i - 1
+        if (!(ok = ptx::mbar_wait(bar_p + 8 * (p & 1), (p >> 1) & 1) && ptx::mbar_wait(bar_v + 8 * v_at, v_phase))) break;
         ptx::tc_fence_after_sync();
-        const uint32_t idesc = ptx::make_idesc_i8(128, kHeadDim, false, true) | (1u << 16);      // u8 x s8, V MN-major
-        const uint64_t dp = ptx::make_kmajor_desc(ptx::smem_addr(sP) + (p & 1) * kP, 512, ptx::kSwizzle64);
-#pragma unroll
-        for (int kk = 0; kk < 2; ++kk) {
-          const uint32_t va = ptx::smem_addr(sV) + (p & 1) * kSlot + kk * 32 * kHeadDim;
-          const uint64_t dv = (uint64_t)((va & 0x3FFFFu) >> 4) | ((uint64_t)(512 >> 4) << 16) | ((uint64_t)(512 >> 4) << 32) |
-                              ((uint64_t)1 << 46) | ((uint64_t)ptx::kSwizzle64 << 61);
-          ptx::mma_i8_ss(tmem + kKeys, dp + 2 * kk, dv, idesc, p + kk > 0 ? 1u : 0u);
-        }
-        ptx::mma_commit(bar_pv + 8 * (p & 1));
+        const uint64_t dpi = dp + (uint64_t)(p & 1) * (kP >> 4), dvi = dv + (uint64_t)v_at * (kSlot >> 4);
+        ptx::mma_i8_ss(tmem + kKeys, dpi, dvi, idesc, p > 0 ? 1u : 0u);
+        ptx::mma_i8_ss(tmem + kKeys, dpi + 2, dvi + ((32 * kHeadDim) >> 4), idesc, 1u);
+        if (p == nt - 1) ptx::mma_commit(bar_pv);
+        if (++v_at == kVRing) { v_at = 0; v_phase ^= 1; }
       }
-      __syncwarp();
-      if (p > 0 && p + 1 < nt) {                   // V of tile p - 1 has been read: the next one takes its place
-        ok = wait(bar_pv + 8 * ((p - 1) & 1), (p - 1) >> 1);
-        if (!ok) break;
-        if (ptx::elect_one()) load_v(p + 1);
-        __syncwarp();
-        ++v_loads;
+      if (!ok) {                                   // copies still in flight land before the shared memory is given up
+        for (int s = max(k_loads - 2, 0); s < k_loads; ++s) ptx::mbar_wait(bar_k + 8 * (s & 1), (s >> 1) & 1);
+        for (int i = max(v_loads - kVRing, 0); i < v_loads; ++i) ptx::mbar_wait(bar_v + 8 * (i % kVRing), (i / kVRing) & 1);
+        ptx::mbar_wait(bar_q, 0);
       }
     }
-    if (!ok) {                                     // copies still in flight land before the shared memory is given up
-      for (int s = max(k_loads - 2, 0); s < k_loads; ++s) ptx::mbar_wait(bar_k + 8 * (s & 1), (s >> 1) & 1);
-      for (int i = max(v_loads - 2, 0); i < v_loads; ++i) ptx::mbar_wait(bar_v + 8 * (i & 1), (i >> 1) & 1);
-      ptx::mbar_wait(bar_q, 0);
-    }
+    ok = __all_sync(0xffffffffu, ok);
   } else if (nt > 0) {
-    // ---- pass A: row maxima, 128 keys at a time
+    // ---- pass A: row maxima, 128 keys at a time (SPLIT 2: one tile of a pair per thread)
+    const int half = warp >> 2;
     int32_t mx = INT32_MIN;
+    auto join = [&](int32_t v, auto op) {          // of a row's two threads
+      if constexpr (SPLIT == 1) return v;
+      s_join[tid] = v;
+      ptx::named_bar_sync(1, 32 * kRowWarps);
+      v = op(s_join[r], s_join[128 + r]);
+      ptx::named_bar_sync(1, 32 * kRowWarps);
+      return v;
+    };
     auto arrive = [&](uint32_t bar) {              // of this warp, after what its lanes did with tensor or shared memory
       ptx::tc_fence_before_sync();
       __syncwarp();
@@ -260,7 +244,7 @@ attention_window_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
       if (!ok) break;
       ptx::tc_fence_after_sync();
 #pragma unroll 1
-      for (int h = 0; h < 2 && 2 * u + h < nt; ++h) {
+      for (int h = SPLIT == 1 ? 0 : half; h < (SPLIT == 1 ? 2 : half + 1) && 2 * u + h < nt; ++h) {
         uint32_t v[64];
         ptx::tmem_ld64(t_row + h * kKeys, v);
         ptx::tmem_wait_ld();
@@ -276,6 +260,8 @@ attention_window_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
       }
       arrive(bar_free);
     }
+
+    mx = join(mx, [](int32_t x, int32_t y) { return max(x, y); });
 
     // ---- pass B: weights, O = sum w v
     const LongAttnConsts& k = a.k;
@@ -297,11 +283,12 @@ attention_window_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
       const uint64_t m = whole(i) ? ~0ull : mask_of(i);
       uint8_t* p_row = sP + (i & 1) * kP + r * kKeys;
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
+      for (int u = 0; u < 2 / SPLIT; ++u) {
+        const int h = SPLIT == 1 ? u : half;
         uint32_t v[32], w[8];
         ptx::tmem_ld32(t_row + 32 * h, v);
         ptx::tmem_wait_ld();
-        if (h == 1) arrive(bar_free);
+        if (u == 2 / SPLIT - 1) arrive(bar_free);
 #pragma unroll
         for (int j = 0; j < 8; ++j)
           w[j] = __byte_perm(__byte_perm(weight(v[4 * j]), weight(v[4 * j + 1]), 0x0073),
@@ -313,28 +300,24 @@ attention_window_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
         }
 #pragma unroll
         for (int j = 0; j < 8; ++j) sum = __dp4a(w[j], 0x01010101u, sum);
-        if (h == 0 && i > 1) {                     // the product before the last has read this buffer
-          ok = wait(bar_pv + 8 * (i & 1), (i - 2) >> 1);
-          if (!ok) break;
-        }
 #pragma unroll
         for (int c = 0; c < 2; ++c)
           *reinterpret_cast<uint4*>(p_row + (((2 * h + c) ^ ((r >> 1) & 3)) << 4)) =
               make_uint4(w[4 * c], w[4 * c + 1], w[4 * c + 2], w[4 * c + 3]);
       }
-      if (!ok) break;
       ptx::fence_proxy_async_smem();
       arrive(bar_p + 8 * (i & 1));
     }
-    if (ok) ok = wait(bar_pv + 8 * ((nt - 1) & 1), (nt - 1) >> 1);
+    if (ok) ok = wait(bar_pv, 0);
 
     // ---- the weighted mean of this row
+    sum = (uint32_t)join((int32_t)sum, [](int32_t x, int32_t y) { return x + y; });
     if (ok) {
       ptx::tc_fence_after_sync();
       const RowShare share = row_share(sum, k);
       int8_t* o = a.out + ((int64_t)row * a.heads + head) * kHeadDim;
 #pragma unroll 1
-      for (int h = 0; h < 2; ++h) {
+      for (int h = SPLIT == 1 ? 0 : half; h < (SPLIT == 1 ? 2 : half + 1); ++h) {
         uint32_t v[32];
         ptx::tmem_ld32(t_row + kKeys + 32 * h, v);
         ptx::tmem_wait_ld();
@@ -379,9 +362,11 @@ int launch_attention_window(ibert_ctx* ctx, const int8_t* qkv, const int32_t* cu
   const int64_t grid = (int64_t)a.tiles * heads;
   if (grid > INT32_MAX) return IBERT_ERR_SHAPE;
   const int mode = !iexp_takes_folded(k.e) ? 2 : (k.e.s_in == 0 ? 0 : 1);
-  auto kernel = mode == 2 ? attention_window_kernel<2> : mode == 1 ? attention_window_kernel<1> : attention_window_kernel<0>;
-  static bool set[kMaxDevices][3] = {{false}};
-  bool& done = set[ctx->device % kMaxDevices][mode];
+  const bool split = grid <= 2 * (int64_t)ctx->num_sms;
+  auto kernel = split ? (mode == 2 ? attention_window_kernel<2, 2> : mode == 1 ? attention_window_kernel<1, 2> : attention_window_kernel<0, 2>)
+                      : (mode == 2 ? attention_window_kernel<2, 1> : mode == 1 ? attention_window_kernel<1, 1> : attention_window_kernel<0, 1>);
+  static bool set[kMaxDevices][6] = {{false}};
+  bool& done = set[ctx->device % kMaxDevices][mode + (split ? 3 : 0)];
   if (!done) {
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kWinSmem) != cudaSuccess) {
       cudaGetLastError();
@@ -389,7 +374,7 @@ int launch_attention_window(ibert_ctx* ctx, const int8_t* qkv, const int32_t* cu
     }
     done = true;
   }
-  return launch_pdl(kernel, dim3((unsigned)grid), dim3(kWinThreads), (size_t)kWinSmem, ctx->stream, 1, mq, mkv, a);
+  return launch_pdl(kernel, dim3((unsigned)grid), dim3(split ? 288 : 160), (size_t)kWinSmem, ctx->stream, 1, mq, mkv, a);
 }
 
 }  // namespace ibert
