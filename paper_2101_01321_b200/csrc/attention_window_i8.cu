@@ -28,9 +28,9 @@ namespace {
 
 constexpr int kKeys = 64;                          // keys per tile
 constexpr int kSlot = kKeys * kHeadDim;            // 4 KB
-constexpr int kVRing = 3;                          // V tiles in shared memory
+constexpr int kKRing = 4, kVRing = 3;              // tiles in shared memory
 constexpr int kP = 128 * kKeys;                    // weights of a tile: 8 KB
-constexpr int kWinSmem = 128 * kHeadDim + 4 * kSlot + kVRing * kSlot + 2 * kP + 256 + 2 * 128 * 4 + 1024;
+constexpr int kWinSmem = 128 * kHeadDim + kKRing * kSlot + kVRing * kSlot + 2 * kP + 256 + 2 * 128 * 4 + 1024;
 
 struct WindowArgs {
   const int32_t* cu;                               // [B + 1]
@@ -61,17 +61,17 @@ attention_window_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint8_t* sQ = smem;                              // [128][64 B], 64-byte swizzle
-  uint8_t* sK = sQ + 128 * kHeadDim;               // two pairs of tiles [64][64 B], 64-byte swizzle
-  uint8_t* sV = sK + 4 * kSlot;                    // kVRing tiles
+  uint8_t* sK = sQ + 128 * kHeadDim;               // kKRing tiles [64][64 B], 64-byte swizzle
+  uint8_t* sV = sK + kKRing * kSlot;                    // kVRing tiles
   uint8_t* sP = sV + kVRing * kSlot;                    // two of [128][64 B], 64-byte swizzle
   uint64_t* s_bar = reinterpret_cast<uint64_t*>(sP + 2 * kP);
-  const uint32_t bar_q = ptx::smem_addr(s_bar), bar_k = bar_q + 8, bar_v = bar_q + 24;       // copies: Q, pairs of K tiles, V tiles
-  const uint32_t bar_s = bar_q + 48, bar_free = bar_q + 56;          // scores complete; scores read by the warps of the rows
-  const uint32_t bar_p = bar_q + 64, bar_pv = bar_q + 80;            // weights written (two buffers); the last product done
-  uint32_t* s_tmem = reinterpret_cast<uint32_t*>(s_bar + 11);
+  const uint32_t bar_q = ptx::smem_addr(s_bar), bar_k = bar_q + 8, bar_v = bar_k + 8 * kKRing;       // copies: Q, K and V tiles
+  const uint32_t bar_s = bar_v + 8 * kVRing, bar_free = bar_s + 16;  // scores complete; scores read by the rows' warps (two buffers)
+  const uint32_t bar_p = bar_free + 16, bar_pv = bar_p + 16;         // weights written (two buffers); the last product done
+  uint32_t* s_tmem = reinterpret_cast<uint32_t*>(s_bar + 15);
   constexpr int kRowWarps = 4 * SPLIT;
   int32_t* s_join = reinterpret_cast<int32_t*>(s_bar + 32);    // [2][128] what the two threads of a row exchange
-  int32_t* s_bounds = reinterpret_cast<int32_t*>(s_bar + 12);  // first visible key, first row of the sequence, last row's first key
+  int32_t* s_bounds = reinterpret_cast<int32_t*>(s_bar + 16);  // first visible key, first row of the sequence, last row's first key
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, r = tid & 127;
   const int head = (int)blockIdx.x % a.heads;
@@ -79,11 +79,13 @@ attention_window_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
   if (warp == 0) {
     if (ptx::elect_one()) {
       ptx::mbar_init(bar_q, 1);
-      for (int i = 0; i < 2; ++i) ptx::mbar_init(bar_k + 8 * i, 1);
+      for (int i = 0; i < kKRing; ++i) ptx::mbar_init(bar_k + 8 * i, 1);
       for (int i = 0; i < kVRing; ++i) ptx::mbar_init(bar_v + 8 * i, 1);
-      ptx::mbar_init(bar_s, 1);
-      ptx::mbar_init(bar_free, kRowWarps);
-      for (int i = 0; i < 2; ++i) ptx::mbar_init(bar_p + 8 * i, kRowWarps);
+      for (int i = 0; i < 2; ++i) {
+        ptx::mbar_init(bar_s + 8 * i, 1);
+        ptx::mbar_init(bar_free + 8 * i, kRowWarps);
+        ptx::mbar_init(bar_p + 8 * i, kRowWarps);
+      }
       ptx::mbar_init(bar_pv, 1);
       ptx::fence_mbar_init();
       ptx::tma_prefetch_desc(&map_q);
@@ -127,7 +129,7 @@ attention_window_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
   // ---- tiles of 64 keys: `lead` over the sinks of the first row's sequence, then from the first row's window on
   const int sink_end = a.window > 0 ? (int)min((int64_t)seq0 + a.sinks, (int64_t)key_w) : seq0;
   const int lead = any ? (sink_end - seq0 + kKeys - 1) / kKeys : 0;
-  const int nt = any ? lead + (min(q0 + 128, a.T) - key_w + kKeys - 1) / kKeys : 0, np = (nt + 1) / 2;
+  const int nt = any ? lead + (min(q0 + 128, a.T) - key_w + kKeys - 1) / kKeys : 0;
   auto base_of = [&](int i) { return i < lead ? seq0 + i * kKeys : key_w + (i - lead) * kKeys; };
   auto mask_of = [&](int i) {
     const int j0 = base_of(i);
@@ -143,12 +145,10 @@ attention_window_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
 
   const int kvh = head / (a.heads / a.kv_heads);
   const int col_k = (a.heads + kvh) * kHeadDim, col_v = col_k + a.kv_heads * kHeadDim;
-  auto load_k = [&](int s) {                       // pair s of pass A, then of pass B
-    const int i = 2 * (s < np ? s : s - np);
-    const uint32_t bar = bar_k + 8 * (s & 1), dst = ptx::smem_addr(sK) + (s & 1) * 2 * kSlot;
-    ptx::mbar_arrive_expect_tx(bar, i + 1 < nt ? 2 * kSlot : kSlot);
-    ptx::tma_load_2d(dst, &map_kv, bar, col_k, base_of(i));
-    if (i + 1 < nt) ptx::tma_load_2d(dst + kSlot, &map_kv, bar, col_k, base_of(i + 1));
+  auto load_k = [&](int s) {                       // tile s of pass A, then of pass B
+    const uint32_t bar = bar_k + 8 * (s % kKRing);
+    ptx::mbar_arrive_expect_tx(bar, kSlot);
+    ptx::tma_load_2d(ptx::smem_addr(sK) + (s % kKRing) * kSlot, &map_kv, bar, col_k, base_of(s < nt ? s : s - nt));
   };
   auto load_v = [&](int i) {
     const int at = i % kVRing;
@@ -159,36 +159,39 @@ attention_window_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
     return __all_sync(0xffffffffu, ptx::mbar_wait(bar, (uint32_t)use & 1u)) != 0;
   };
   const uint64_t dq = ptx::make_kmajor_desc(ptx::smem_addr(sQ), 512, ptx::kSwizzle64);
-  auto score_mma = [&](uint32_t k_addr, int n) {   // S = Q K^T over n keys: 64 dimensions are two K steps
-    const uint32_t idesc = ptx::make_idesc_i8(128, n, true, true);
-    const uint64_t dk = ptx::make_kmajor_desc(k_addr, 512, ptx::kSwizzle64);
-    ptx::mma_i8_ss(tmem, dq, dk, idesc, 0u);
-    ptx::mma_i8_ss(tmem, dq + 2, dk + 2, idesc, 1u);
-    ptx::mma_commit(bar_s);
+  const uint64_t dk0 = ptx::make_kmajor_desc(ptx::smem_addr(sK), 512, ptx::kSwizzle64);
+  auto score_mma = [&](int s, int buffer) {        // S = Q K^T of tile s of the passes: 64 dimensions are two K steps
+    const uint32_t idesc = ptx::make_idesc_i8(128, kKeys, true, true);
+    const uint64_t dk = dk0 + (uint64_t)(s % kKRing) * (kSlot >> 4);
+    ptx::mma_i8_ss(tmem + buffer * kKeys, dq, dk, idesc, 0u);
+    ptx::mma_i8_ss(tmem + buffer * kKeys, dq + 2, dk + 2, idesc, 1u);
+    ptx::mma_commit(bar_s + 8 * buffer);
   };
+  // pass A: tile i in buffer i & 1; pass B: every tile in buffer 0, which pass A has used n0 times (buffer 1 holds the context)
+  const int n0 = (nt + 1) / 2;
 
   bool ok = true;
   if (nt > 0 && warp == kRowWarps) {
-    // ---- copies and matrix products, all by one thread.  Score tile u (pass A: pairs of tiles 0 .. np - 1, pass B: tiles np ..)
-    // may be issued when the rows have read the one before; a pair of K tiles is replaced when its last scores have been read.
+    // ---- copies and matrix products, all by one thread.  A tile's scores may be issued when the rows have read what was in
+    // its buffer; those read are complete, as are all before them, and their K tiles may be replaced.
     // Products complete in the order of their issue, and their barrier counts all that were issued before: scores that have
     // been read say that the product of weights issued before them has read its weights and values, too.  (The values need
     // three tiles, the weights two, for that; waits of their own for either cost this thread more than a step takes.)
     if (ptx::elect_one()) {
-      int k_loads = min(2, 2 * np), v_loads = min(kVRing, nt);
+      int k_loads = min(kKRing, 2 * nt), v_loads = min(kVRing, nt);
       ptx::mbar_arrive_expect_tx(bar_q, 128 * kHeadDim);
       ptx::tma_load_2d(ptx::smem_addr(sQ), &map_q, bar_q, head * kHeadDim, q0);
       for (int s = 0; s < k_loads; ++s) load_k(s);
       for (int i = 0; i < v_loads; ++i) load_v(i);
       ok = ptx::mbar_wait(bar_q, 0);
-      for (int u = 0; u < np && ok; ++u) {
-        if (u > 0) {
-          if (!(ok = ptx::mbar_wait(bar_free, (u - 1) & 1))) break;
-          if (k_loads < 2 * np) load_k(k_loads++);
+      for (int i = 0; i < nt && ok; ++i) {
+        if (i > 1) {
+          if (!(ok = ptx::mbar_wait(bar_free + 8 * (i & 1), ((i >> 1) - 1) & 1))) break;
+          if (k_loads < 2 * nt) load_k(k_loads++);           // tile i + 2 in the place of tile i - 2
         }
-        if (!(ok = ptx::mbar_wait(bar_k + 8 * (u & 1), (u >> 1) & 1))) break;
+        if (!(ok = ptx::mbar_wait(bar_k + 8 * (i % kKRing), (i / kKRing) & 1))) break;
         ptx::tc_fence_after_sync();
-        score_mma(ptx::smem_addr(sK) + (u & 1) * 2 * kSlot, 2 * u + 1 < nt ? 128 : 64);
+        score_mma(i, i & 1);
       }
       const uint32_t idesc = ptx::make_idesc_i8(128, kHeadDim, false, true) | (1u << 16);        // u8 x s8, V MN-major
       const uint64_t dp = ptx::make_kmajor_desc(ptx::smem_addr(sP), 512, ptx::kSwizzle64);
@@ -197,12 +200,12 @@ attention_window_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
       int v_at = 0, v_phase = 0;                   // of tile i - 1
       for (int i = 0; i <= nt && ok; ++i) {
         if (i < nt) {                              // scores of tile i
-          const int s = np + (i >> 1);
-          if (!(ok = ptx::mbar_wait(bar_free, (np + i - 1) & 1))) break;
-          if (!(i & 1) && !(ok = ptx::mbar_wait(bar_k + 8 * (s & 1), (s >> 1) & 1))) break;
+          const int s = nt + i;
+          if (!(ok = ptx::mbar_wait(bar_free, (n0 + i - 1) & 1) && ptx::mbar_wait(bar_k + 8 * (s % kKRing), (s / kKRing) & 1))) break;
           ptx::tc_fence_after_sync();
-          score_mma(ptx::smem_addr(sK) + (s & 1) * 2 * kSlot + (i & 1) * kSlot, 64);
-          if (!(i & 1) && k_loads < 2 * np) load_k(k_loads++);
+          score_mma(s, 0);
+          // (the scores that buffer 0 held were those of tile s - 1, at the start of the pass s - 2 if not s - 1)
+          for (const int to = min(s + (i > 0 ? 3 : 2), 2 * nt - 1); k_loads <= to;) load_k(k_loads++);
           if (i >= kVRing) { load_v(i); ++v_loads; }
         }
         if (i == 0) continue;
@@ -216,14 +219,14 @@ attention_window_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
         if (++v_at == kVRing) { v_at = 0; v_phase ^= 1; }
       }
       if (!ok) {                                   // copies still in flight land before the shared memory is given up
-        for (int s = max(k_loads - 2, 0); s < k_loads; ++s) ptx::mbar_wait(bar_k + 8 * (s & 1), (s >> 1) & 1);
+        for (int s = max(k_loads - kKRing, 0); s < k_loads; ++s) ptx::mbar_wait(bar_k + 8 * (s % kKRing), (s / kKRing) & 1);
         for (int i = max(v_loads - kVRing, 0); i < v_loads; ++i) ptx::mbar_wait(bar_v + 8 * (i % kVRing), (i / kVRing) & 1);
         ptx::mbar_wait(bar_q, 0);
       }
     }
     ok = __all_sync(0xffffffffu, ok);
   } else if (nt > 0) {
-    // ---- pass A: row maxima, 128 keys at a time (SPLIT 2: one tile of a pair per thread)
+    // ---- pass A: row maxima
     const int half = warp >> 2;
     int32_t mx = INT32_MIN;
     auto join = [&](int32_t v, auto op) {          // of a row's two threads
@@ -239,28 +242,27 @@ attention_window_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
       __syncwarp();
       if (lane == 0) ptx::mbar_arrive(bar);
     };
-    for (int u = 0; u < np; ++u) {
-      ok = wait(bar_s, u);
+    for (int i = 0; i < nt; ++i) {
+      ok = wait(bar_s + 8 * (i & 1), i >> 1);
       if (!ok) break;
       ptx::tc_fence_after_sync();
-#pragma unroll 1
-      for (int h = SPLIT == 1 ? 0 : half; h < (SPLIT == 1 ? 2 : half + 1) && 2 * u + h < nt; ++h) {
-        uint32_t v[64];
-        ptx::tmem_ld64(t_row + h * kKeys, v);
-        ptx::tmem_wait_ld();
-        if (!whole(2 * u + h)) {
-          const uint64_t m = mask_of(2 * u + h);
-          const uint32_t m0 = (uint32_t)m, m1 = (uint32_t)(m >> 32);
+      constexpr int kCols = kKeys / SPLIT;
+      const int first_col = SPLIT == 1 ? 0 : half * kCols;
+      uint32_t v[kCols];
+      if constexpr (SPLIT == 1) ptx::tmem_ld64(t_row + (i & 1) * kKeys, v);
+      else ptx::tmem_ld32(t_row + (i & 1) * kKeys + first_col, v);
+      ptx::tmem_wait_ld();
+      arrive(bar_free + 8 * (i & 1));
+      if (!whole(i)) {
+        const uint64_t m = mask_of(i) >> first_col;
+        const uint32_t m0 = (uint32_t)m, m1 = (uint32_t)(m >> 32);
 #pragma unroll
-          for (int j = 0; j < 64; ++j)
-            if (!(((j < 32 ? m0 : m1) >> (j & 31)) & 1u)) v[j] = (uint32_t)INT32_MIN;
-        }
-#pragma unroll
-        for (int j = 0; j < 64; j += 2) mx = __vimax3_s32(mx, (int32_t)v[j], (int32_t)v[j + 1]);
+        for (int j = 0; j < kCols; ++j)
+          if (!(((j < 32 ? m0 : m1) >> (j & 31)) & 1u)) v[j] = (uint32_t)INT32_MIN;
       }
-      arrive(bar_free);
+#pragma unroll
+      for (int j = 0; j < kCols; j += 2) mx = __vimax3_s32(mx, (int32_t)v[j], (int32_t)v[j + 1]);
     }
-
     mx = join(mx, [](int32_t x, int32_t y) { return max(x, y); });
 
     // ---- pass B: weights, O = sum w v
@@ -277,7 +279,7 @@ attention_window_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
     };
     uint32_t sum = 0;
     for (int i = 0; i < nt && ok; ++i) {
-      ok = wait(bar_s, np + i);
+      ok = wait(bar_s, n0 + i);
       if (!ok) break;
       ptx::tc_fence_after_sync();
       const uint64_t m = whole(i) ? ~0ull : mask_of(i);
