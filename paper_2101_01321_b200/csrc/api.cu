@@ -1200,6 +1200,7 @@ static int make_long_attn_consts(double S_q, double S_k, double S_v, double S_ct
   if (k->e.q_ln2 <= 2 || k->e.wide_post < 0) return IBERT_ERR_SCALE_RANGE;    // the unclamped quotient is not available
   const uint32_t top = (uint32_t)((int64_t)k->e.q_b * k->e.q_b + k->e.q_c) >> k->e.s_out;
   k->b_w = ((uint32_t)p_max << 24) / top;
+  make_short_quotient(k);
   return dyadic(S_v / S_ctx, &k->b, &k->c);
 }
 

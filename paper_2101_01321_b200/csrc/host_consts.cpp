@@ -158,6 +158,26 @@ int make_exp_consts(double S, int p_max, ExpConsts* k) {
   return IBERT_OK;
 }
 
+// Rounded up, m = ceil(2^k / q) with m q = 2^k + e0 is exact for D while D e0 < 2^k; rounded down, m q = 2^k - e1, for D + 1
+// in the place of D while (D + 1) e1 <= 2^k.
+void make_short_quotient(LongAttnConsts* k) {
+  k->short_m = 0;
+  k->short_k = k->short_add = 0;
+  const uint64_t q = k->e.q_ln2, top = 9 * q;
+  if (k->e.s_in != 0) return;
+  for (int s = 27; s >= 16; --s) {
+    const uint64_t p = uint64_t(1) << s, up = (p + q - 1) / q, down = p / q;
+    for (int add = 0; add < 2; ++add) {
+      const uint64_t m = add ? down : up, e = add ? p - down * q : up * q - p;
+      if ((top + add) * e + (add ? 0 : 1) > p || (add && e == 0) || (top + add) * m + ((uint64_t)k->e.s_out << s) >= (uint64_t(1) << 32)) continue;
+      k->short_m = (uint32_t)m;
+      k->short_k = s;
+      k->short_add = add;
+      return;
+    }
+  }
+}
+
 // Multipliers of the per-head norm: gamma 128 / S_out in units of 2^-g, 16 bits, g common to the head (at most 16; below -8
 // the shift of the kernel would leave its range).
 int make_head_norm(const double* gamma, double S_out, int16_t* b, int32_t* g) {

@@ -304,7 +304,13 @@ struct LongAttnConsts {
   ExpConsts e;
   uint32_t b_w;
   int32_t b, c;
+  // the quotient of Algorithm 3 in 32 bits: from a distance of 9 q_ln2 on the weight is 0, and for d <= 9 q_ln2
+  // (d + short_add) short_m >> short_k = floor(d / q_ln2), the product and s_out 2^short_k together below 2^32.
+  // short_k = 0: not available (a pre-shift, or q_ln2 above some 5000)
+  uint32_t short_m;
+  int32_t short_k, short_add;
 };
+void make_short_quotient(LongAttnConsts* k);
 constexpr int kMaxVisible = 65536;       // visible keys per query: 255 * 128 * 65536 < 2^31
 
 int launch_attention_decode(ibert_ctx* ctx, const int8_t* q, const int8_t* k_cache, const int8_t* v_cache,
