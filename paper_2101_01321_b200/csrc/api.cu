@@ -1285,6 +1285,13 @@ int ibert_selftest_exp_division(double S, int32_t* q_ln2_out) {
     const uint32_t nf = zf + (uint32_t)k.s_out;
     if ((nf > 31 ? 0u : (uint32_t)(tf * tf + k.q_c) >> nf) != (n > 31 ? 0u : (uint32_t)(t * t + k.q_c) >> n)) return IBERT_ERR_VALUE_RANGE;
   }
+  LongAttnConsts lk{};
+  static_cast<ExpConsts&>(lk.e) = k;
+  make_short_quotient(&lk);
+  for (uint32_t d = 0; lk.short_k && d <= 9 * k.q_ln2; ++d) {   // quotient and post-shift of the windowed attention, in 32 bits
+    const uint32_t n = ((d + (uint32_t)lk.short_add) * lk.short_m + ((uint32_t)k.s_out << lk.short_k)) >> lk.short_k;
+    if (n != d / k.q_ln2 + (uint32_t)k.s_out) return IBERT_ERR_VALUE_RANGE;
+  }
   if (k.wide_post >= 0) {            // the unclamped form used on attention scores: every d < 2^21
     for (uint32_t d = 0; d < (1u << 21); ++d) {
       const uint32_t z = (uint32_t)(((uint64_t)d * (uint64_t)k.wide_m) >> 32) >> k.wide_post;

@@ -88,7 +88,6 @@ attention_decode_kernel(const __grid_constant__ DecodeArgs a) {
 
   for (int i = tid; i < kMaxGroup * kHeadDim; i += kThreads) (&s_out[0][0])[i] = 0;
   if (tid < kMaxGroup) s_sum[tid] = 0;
-  ptx::grid_dep_launch();
   ptx::grid_dep_wait();
 
   // ---- visible keys: j < first and start <= j < len, in tiles of 32: `lead` tiles in front of the window's first one
@@ -306,6 +305,7 @@ attention_decode_kernel(const __grid_constant__ DecodeArgs a) {
       if (2 * t + (c & 1) < G) atomicAdd(&s_out[4 * i + c][lane], acc[i][c]);
   if (cl > 1) ptx::cluster_sync(); else __syncthreads();
 
+  ptx::grid_dep_launch();                // (not earlier: CTAs of the next kernel would wait in the slots of this one's last ones)
   // ---- every CTA joins and divides its part of the G x 64 results
   for (int i = (int)rank * kThreads + tid; i < G * kHeadDim; i += cl * kThreads) {
     const int h = i / kHeadDim, d = i % kHeadDim;

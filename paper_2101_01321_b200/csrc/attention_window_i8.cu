@@ -97,7 +97,6 @@ attention_window_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
     ptx::tmem_alloc(ptx::smem_addr(s_tmem), 128);
     ptx::tmem_relinquish();
   }
-  ptx::grid_dep_launch();
   ptx::grid_dep_wait();
 
   // ---- this row's sequence: the last b with cu[b] <= row, searched 32-fold for the warp's first row, on from there
@@ -347,6 +346,9 @@ attention_window_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
       }
     }
   }
+  // (Not earlier: CTAs of the next kernel that wait for this one would take the slots that its own last CTAs are balanced by,
+  // and be stacked on the SMs that happen to have one free.)
+  ptx::grid_dep_launch();
   if (!ok) atomicCAS(a.status, 0, IBERT_ERR_TIMEOUT);
   if (bad) atomicCAS(a.status, 0, IBERT_ERR_VALUE_RANGE);
   ptx::tc_fence_before_sync();
@@ -374,7 +376,7 @@ int launch_attention_window(ibert_ctx* ctx, const int8_t* qkv, const int32_t* cu
   const int64_t grid = (int64_t)a.tiles * heads;
   if (grid > INT32_MAX) return IBERT_ERR_SHAPE;
   const int mode = k.short_k ? 3 : (!iexp_takes_folded(k.e) ? 2 : (k.e.s_in == 0 ? 0 : 1));
-  const bool split = grid <= 2 * (int64_t)ctx->num_sms;
+  const bool split = grid <= 4 * (int64_t)ctx->num_sms;
   decltype(&attention_window_kernel<0, 1>) const kernels[2][4] = {
       {attention_window_kernel<0, 1>, attention_window_kernel<1, 1>, attention_window_kernel<2, 1>, attention_window_kernel<3, 1>},
       {attention_window_kernel<0, 2>, attention_window_kernel<1, 2>, attention_window_kernel<2, 2>, attention_window_kernel<3, 2>}};

@@ -66,7 +66,6 @@ qkv_rope_kernel(const __grid_constant__ RopeArgs a) {
   const int heads_all = a.heads + 2 * a.kv_heads;
   const int64_t item = (int64_t)blockIdx.x * (kRopeThreads / 32) + (threadIdx.x >> 5);
   const uint32_t group = ((1u << kLanes) - 1u) << (threadIdx.x & (32 - kLanes));
-  ptx::grid_dep_launch();
   ptx::grid_dep_wait();
   const int64_t t_group = item / a.chunks, t = t_group * N + (threadIdx.x & 31) / kLanes;
   if (t >= a.T) return;                                      // (whole groups of lanes; shuffles stay within one)

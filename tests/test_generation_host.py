@@ -108,6 +108,11 @@ def test_no_rows_are_no_work(lib):
     assert _window(lib, B=0, T=5) == 0
 
 
+@pytest.mark.parametrize("S", [0.2, 0.05, 7.3e-3, 1.1e-3, 4e-4, 2.5e-4, 1.77e-4, 1.2e-4, 9e-5, 5e-5, 3e-5, 1e-6, 1.25e-9])
+def test_quotients_of_the_exponential_hold_for_every_distance(lib, S):
+    assert lib.ibert_selftest_exp_division(S, None) == 0
+
+
 # ----------------------------------------------------------------------------- rotation tables
 @pytest.mark.parametrize("rot", [8, 16, 48, 64])
 @pytest.mark.parametrize("pos0,n,factor", [(0, 50, 1.0), (131000, 9, 1.0), (7, 3, 1.37), (5, 0, 1.0)])

@@ -105,7 +105,8 @@ def test_extreme_values():
 
 
 @pytest.mark.parametrize("scales", [(1e-4, 1e-4, 1.0, 1.0), (0.3, 0.3, 1e-6, 1.0), (1.0, 1.0, 5.0, 0.001), (1e-5, 1e-5, 0.02, 0.02),
-                                    (0.9, 0.9, 0.1, 0.1), (0.0123, 0.077, 0.5, 0.25)])
+                                    (0.9, 0.9, 0.1, 0.1), (0.0123, 0.077, 0.5, 0.25),
+                                    (0.02, 0.02, 0.1, 0.1), (0.003, 0.003, 0.1, 0.1), (0.04, 0.02, 0.1, 0.05), (0.35, 0.23, 0.1, 0.1)])
 def test_scales(scales):
     _run(np.random.default_rng(6), [3, 77, 500], 4, 2, 16, scales=scales)
 
