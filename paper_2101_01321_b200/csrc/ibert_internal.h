@@ -336,12 +336,11 @@ struct RopeArgs {
   int32_t* status;
   int64_t T, max_pos, n_slots;
   int32_t heads, kv_heads, rot, interleaved, with_kv, log_page;
-  int32_t per;                           // heads that a group of lanes takes one after the other
-  int32_t chunks, chunks_q, chunks_kv;   // groups of `per` heads: of a token, of Q, of K (and of V); set by the launcher
-  // Q, K without a norm: dyadic(128 S_in / S_out); V: dyadic(S_in / S_v); k = 32 - c, set by the launcher
-  int32_t b[3], c[3], k[3];
+  // heads that a group of lanes takes one after the other, and how many such chunks a token, Q, and K (or V) have; set by the launcher
+  int32_t per_q, per_kv, chunks, chunks_q, chunks_kv;
+  int32_t b[3], c[3];                    // Q, K without a norm: dyadic(128 S_in / S_out); V: dyadic(S_in / S_v)
   int32_t g[2];                          // with a norm: gamma 128 / S_out in units of 2^-g, 16 bits
-  int16_t gamma[2][64];
+  alignas(16) int16_t gamma[2][64];
 };
 int make_head_norm(const double* gamma, double S_out, int16_t* b, int32_t* g);
 int launch_qkv_rope(ibert_ctx* ctx, RopeArgs a, bool x_is_i16, bool norm);

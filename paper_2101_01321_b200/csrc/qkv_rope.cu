@@ -45,16 +45,31 @@ __device__ __forceinline__ void store_run(int8_t* p, const uint32_t* w) {
   else *reinterpret_cast<uint32_t*>(p) = w[0];
 }
 
-// clamp(round(x b / 2^c), +-qmax) of a 16-bit x.  k = 32 - c <= 16: x 2^k fits 32 bits and the result is one upper word.
-__device__ __forceinline__ int32_t requant_16(int32_t x, int32_t b, int c, int k, int64_t half, int32_t qmax) {
-  if (k <= 16) return clamp_sym(requant_upper((int32_t)((uint32_t)x << k), b), qmax);
-  return requant_add(x, b, half, c, qmax);
+// (v b + 2^(sh-1)) >> sh for sh >= 33: the rounding constant is a whole number of upper words, so one multiply-high with an
+// addend leaves nothing to be carried
+__device__ __forceinline__ int32_t requant_high(int32_t v, int32_t b, int32_t add, int shift) {   // 2^(sh-33), sh - 32
+  int32_t d;
+  asm("mad.hi.s32 %0, %1, %2, %3;" : "=r"(d) : "r"(v), "r"(b), "r"(add));
+  return d >> shift;
+}
+// clamp(round(x b / 2^c), +-qmax) of 16-bit values: x 2^16 fits 32 bits
+template <int N>
+__device__ __forceinline__ void requant_16(int32_t* x, int32_t b, int c, int32_t qmax) {
+  if (c >= 17) {
+    const int32_t add = 1 << (c - 17);
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = clamp_sym(requant_high((int32_t)((uint32_t)x[i] << 16), b, add, c - 16), qmax);
+  } else {
+    const int64_t half = rounding_half(c);
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = requant_add(x[i], b, half, c, qmax);
+  }
 }
 
 // 32 / N lanes own one head vector, a lane two runs of N elements such that both elements of every rotated pair are its
 // own: with rotated halves runs N j and rot/2 + N j in lane j, and the dimensions that stay in the lanes behind; interleaved
 // (and without rotation) the 2 N elements from 2 N j.  N = 8 (16-byte loads of Q16, and the root and the reciprocal of a head
-// on four lanes instead of eight) wherever rot is a multiple of 16.  The lanes take `per` heads of one token one after the
+// on four lanes instead of eight) wherever rot is a multiple of 16.  The lanes take several heads of one token one after the
 // other, so that position, slot, cos, sin and the gammas are loaded once for them, with the next head's elements in flight.
 // The N groups of a warp take N tokens and the same heads: Q and K on one side, V on the other do different work, and mixed
 // in a warp they cost half as much again.
@@ -64,17 +79,19 @@ qkv_rope_kernel(const __grid_constant__ RopeArgs a) {
   constexpr int kLanes = 32 / N;
   const int j = threadIdx.x & (kLanes - 1);
   const int heads_all = a.heads + 2 * a.kv_heads;
-  const int64_t item = (int64_t)blockIdx.x * (kRopeThreads / 32) + (threadIdx.x >> 5);
-  const uint32_t group = ((1u << kLanes) - 1u) << (threadIdx.x & (32 - kLanes));
+  const int block_group = (int)blockIdx.x / a.chunks;       // (the parts of a token next to each other)
+  const int64_t t_group = (int64_t)block_group * (kRopeThreads / 32) + (threadIdx.x >> 5);
   ptx::grid_dep_wait();
-  const int64_t t_group = item / a.chunks, t = t_group * N + (threadIdx.x & 31) / kLanes;
-  if (t >= a.T) return;                                      // (whole groups of lanes; shuffles stay within one)
-  int chunk = (int)(item - t_group * a.chunks);
-  // chunks of `per` heads of Q, then of K, then of V
+  const int64_t t_own = t_group * N + (threadIdx.x & 31) / kLanes;
+  if (t_group * N >= a.T) return;                            // (whole warps)
+  const bool live = t_own < a.T;                             // (the others repeat the last token and store nothing)
+  const int64_t t = live ? t_own : a.T - 1;
+  int chunk = (int)blockIdx.x - block_group * a.chunks;
+  // chunks of heads of Q, then of K, then of V
   const int part = chunk < a.chunks_q ? 0 : (chunk < a.chunks_q + a.chunks_kv ? 1 : 2);
   chunk -= part == 0 ? 0 : (part == 1 ? a.chunks_q : a.chunks_q + a.chunks_kv);
   const int n_heads = part == 0 ? a.heads : a.kv_heads;
-  const int h0 = chunk * a.per, h1 = min(h0 + a.per, n_heads);         // within the part
+  const int per = part == 0 ? a.per_q : a.per_kv, h0 = chunk * per, h1 = min(h0 + per, n_heads);         // within the part
   const int head_base = part == 0 ? 0 : (part == 1 ? a.heads : a.heads + a.kv_heads);
 
   const int half = a.rot >> 1;
@@ -104,19 +121,24 @@ qkv_rope_kernel(const __grid_constant__ RopeArgs a) {
     }
   }
   int8_t* cache_row = nullptr;                               // first byte of the token's row of head h0 in its cache
-  if (a.k_cache && part > 0) {
+  if (a.k_cache && part > 0 && live) {
     const int32_t slot = ptx::ld_dep(a.slots + t);
     if (slot >= 0 && slot < a.n_slots) {
       const int64_t page = slot >> a.log_page, row = slot & ((1 << a.log_page) - 1);
       cache_row = (part == 1 ? a.k_cache : a.v_cache) + ((((page * a.kv_heads + h0) << a.log_page) + row) * kHeadDim);
     } else if (slot != -1) bad = true;
   }
-  int8_t* out_row = a.with_kv || part == 0 ? a.out + (t * (a.with_kv ? heads_all : a.heads) + head_base + h0) * kHeadDim : nullptr;
-  const int64_t half_c = rounding_half(a.c[part]);
+  int8_t* out_row = live && (a.with_kv || part == 0) ? a.out + (t * (a.with_kv ? heads_all : a.heads) + head_base + h0) * kHeadDim : nullptr;
   int32_t gam[2 * N];
   if (NORM && part < 2) {
+    uint32_t w0[N / 2], w1[N / 2];
 #pragma unroll
-    for (int i = 0; i < 2 * N; ++i) gam[i] = a.gamma[part][i < N ? e0 + i : e1 + i - N];
+    for (int i = 0; i < N / 2; ++i) {
+      w0[i] = reinterpret_cast<const uint32_t*>(a.gamma[part] + e0)[i];
+      w1[i] = reinterpret_cast<const uint32_t*>(a.gamma[part] + e1)[i];
+    }
+    unpack_run<N, int16_t>(w0, gam);
+    unpack_run<N, int16_t>(w1, gam + N);
   }
 
   for (int h = h0; h < h1; ++h) {
@@ -129,15 +151,14 @@ qkv_rope_kernel(const __grid_constant__ RopeArgs a) {
       load_run<N>(x_row + e1, w1);
     }
     if (part == 2) {
-#pragma unroll
-      for (int i = 0; i < 2 * N; ++i) x[i] = requant_16(x[i], a.b[2], a.c[2], a.k[2], half_c, 127);
+      requant_16<2 * N>(x, a.b[2], a.c[2], 127);
     } else {
       if constexpr (NORM) {
         int64_t ss = 0;
 #pragma unroll
         for (int i = 0; i < 2 * N; ++i) ss += (int64_t)x[i] * x[i];
 #pragma unroll
-        for (int d = 1; d < kLanes; d <<= 1) ss += __shfl_xor_sync(group, ss, d);
+        for (int d = 1; d < kLanes; d <<= 1) ss += __shfl_xor_sync(0xffffffffu, ss, d);
         constexpr int s0 = sizeof(T) == 1 ? 16 : 10;
         // ISqrt(ss 2^s0) = floor(sqrt(floor(ss 2^(s0+2) / 4)))
         const uint32_t r = max(ln_root<3>((uint64_t)ss << (s0 + 2), 4u, 0x80000000u), 1u);
@@ -145,18 +166,17 @@ qkv_rope_kernel(const __grid_constant__ RopeArgs a) {
         const uint32_t y = r << (32 - l);                    // floor(2^(l+29) / r) = floor(2^61 / y)
         uint32_t rho = reciprocal_q31(y) >> 2;
         rho += (uint64_t(1) << 61) - (uint64_t)rho * y >= y ? 1u : 0u;
-        const int64_t add = int64_t(1) << (sh - 1);
-        if (sh >= 32) {                                      // the upper word, shifted on
+        if (__all_sync(0xffffffffu, sh >= 33)) {
+          const int32_t add = 1 << (sh - 33);
 #pragma unroll
-          for (int i = 0; i < 2 * N; ++i)
-            x[i] = clamp_sym(requant_upper_add(x[i] * gam[i], (int32_t)rho, add) >> (sh - 32), 32767);
+          for (int i = 0; i < 2 * N; ++i) x[i] = clamp_sym(requant_high(x[i] * gam[i], (int32_t)rho, add, sh - 32), 32767);
         } else {
+          const int64_t add = int64_t(1) << (sh - 1);
 #pragma unroll
           for (int i = 0; i < 2 * N; ++i) x[i] = requant_add(x[i] * gam[i], (int32_t)rho, add, sh, 32767);
         }
       } else {
-#pragma unroll
-        for (int i = 0; i < 2 * N; ++i) x[i] = requant_16(x[i], a.b[part], a.c[part], a.k[part], half_c, 32767);
+        requant_16<2 * N>(x, a.b[part], a.c[part], 32767);
       }
       if (rotates) {
         if (a.interleaved) {
@@ -202,7 +222,7 @@ template <typename T, bool NORM>
 int launch_typed(ibert_ctx* ctx, const RopeArgs& a) {
   const bool wide = a.rot % 16 == 0;
   const int tokens = wide ? 8 : 4;                 // of a warp
-  const int64_t warps = (a.T + tokens - 1) / tokens * a.chunks, blocks = (warps + kRopeThreads / 32 - 1) / (kRopeThreads / 32);
+  const int64_t per_block = (int64_t)tokens * (kRopeThreads / 32), blocks = (a.T + per_block - 1) / per_block * a.chunks;
   if (blocks > INT32_MAX) return IBERT_ERR_SHAPE;
   return launch_pdl(wide ? qkv_rope_kernel<T, NORM, 8> : qkv_rope_kernel<T, NORM, 4>, dim3((unsigned)blocks), dim3(kRopeThreads), 0,
                     ctx->stream, 1, a);
@@ -211,14 +231,16 @@ int launch_typed(ibert_ctx* ctx, const RopeArgs& a) {
 }  // namespace
 
 int launch_qkv_rope(ibert_ctx* ctx, RopeArgs a, bool x_is_i16, bool norm) {
-  // heads per group of lanes: one while there are fewer heads than lanes on the GPU, up to four beyond
+  // heads per group of lanes: up to eight (what is loaded once per token and part costs half a head), fewer while the groups
+  // would not fill the GPU
   const bool kv = a.with_kv || a.k_cache;
   const int64_t vectors = a.T * (a.heads + (kv ? 2 * a.kv_heads : 0));
-  a.per = (int)std::min<int64_t>(4, std::max<int64_t>(1, vectors / ((int64_t)ctx->num_sms * 512)));
-  a.chunks_q = (a.heads + a.per - 1) / a.per;
-  a.chunks_kv = kv ? (a.kv_heads + a.per - 1) / a.per : 0;
+  const int per = (int)std::min<int64_t>(8, std::max<int64_t>(1, vectors / ((int64_t)ctx->num_sms * 128)));
+  a.chunks_q = (a.heads + per - 1) / per;
+  a.per_q = (a.heads + a.chunks_q - 1) / a.chunks_q;
+  a.chunks_kv = kv ? (a.kv_heads + per - 1) / per : 0;
+  a.per_kv = kv ? (a.kv_heads + a.chunks_kv - 1) / a.chunks_kv : 1;
   a.chunks = a.chunks_q + 2 * a.chunks_kv;
-  for (int i = 0; i < 3; ++i) a.k[i] = 32 - a.c[i];
   a.status = ctx->d_status;
   if (x_is_i16) return norm ? launch_typed<int16_t, true>(ctx, a) : launch_typed<int16_t, false>(ctx, a);
   return norm ? launch_typed<int8_t, true>(ctx, a) : launch_typed<int8_t, false>(ctx, a);
