@@ -402,7 +402,11 @@ int ibert_attention_window_i8(ibert_ctx* ctx, const int8_t* qkv, const int32_t* 
                               double S_v, double S_ctx, int p_max, int8_t* out, double* S_ret);
 
 /* Attention of ONE new token per sequence over the paged cache, which already holds the token's own key and value:
-   q int8 [B][heads 64] at S_q, out int8 [B][heads 64] at S_ctx (*S_ret).  lens: device int32 [B], tokens in the cache
+   q int8 [rows][heads 64] at S_q, out int8 [rows][heads 64] at S_ctx (*S_ret).  cu_seqlens NULL: row b belongs to sequence
+   b, and rows = B.  Else (device int32 [B+1], what ibert_kv_slots gives for a step in which some requests get no token, have
+   ended or got a whole prompt) sequence b's row is cu_seqlens[b+1] - 1, its last new token; the rows of other tokens, and
+   all rows of a sequence with no new token, are left as they were; a row outside [0, rows) is left out and records
+   IBERT_ERR_VALUE_RANGE.  lens: device int32 [B], tokens in the cache
    (the new one included), at most max_len; a sequence of length 0 yields 0.  Key j is visible if j < lens[b] and
    (window = 0, or j >= lens[b] - window, or j < sinks): a sliding window, and first tokens that stay visible.  Pages
    that hold no visible key are not looked at.  With e_j the i-exp (Algorithm 3) of the distance of s_j = q k_j (scale
@@ -412,13 +416,14 @@ int ibert_attention_window_i8(ibert_ctx* ctx, const int8_t* qkv, const int32_t* 
    -- weights relative to the row's maximum, divided by their sum at the end.  (ibert_attention_i8 divides first; over
    thousands of keys all of its u8 probabilities would be 0.)
    At most 65536 visible keys: min(max_len, window + sinks if window > 0) <= 65536, else IBERT_ERR_SHAPE; window, sinks >= 0;
-   max_len <= max_pages * page_size.  A length above max_len (taken as max_len) or below 0, and a visible key on a page
+   max_len <= max_pages * page_size, max_len < 2^31 - 256, rows * heads < 2^31.  A length above max_len (taken as max_len) or below 0, and a visible key on a page
    outside [0, n_pages) (the key is left out), record IBERT_ERR_VALUE_RANGE in the context's status.
    IBERT_ERR_SCALE_RANGE also for score scales so coarse that floor(ln2 / (S_q S_k / 8)) <= 2; p_max in {255, 127}. */
 int ibert_attention_decode_i8(ibert_ctx* ctx, const int8_t* q, const int8_t* k_cache, const int8_t* v_cache,
-                              const int32_t* block_tables, const int32_t* lens, int B, int max_len, int max_pages,
-                              int64_t n_pages, int page_size, int heads, int kv_heads, int window, int sinks, double S_q,
-                              double S_k, double S_v, double S_ctx, int p_max, int8_t* out, double* S_ret);
+                              const int32_t* block_tables, const int32_t* lens, const int32_t* cu_seqlens, int64_t rows,
+                              int B, int max_len, int max_pages, int64_t n_pages, int page_size, int heads, int kv_heads,
+                              int window, int sinks, double S_q, double S_k, double S_v, double S_ctx, int p_max, int8_t* out,
+                              double* S_ret);
 
 /* ---- h-GELU, the comparison function of the paper (Eq. 6; Table 1, Table 3) --------------------
    h-GELU(x) = x ReLU6(1.702 x + 3) / 6.  The paper notes that it can be computed with integers

@@ -114,7 +114,7 @@ def lib():
         L.ibert_rope_frequencies.argtypes = [i32, dbl, dbl, dbl, dbl, dbl, vp]
         L.ibert_rope_rows.argtypes = [vp, i32, i64, i64, dbl, vp]
         L.ibert_qkv_rope_i8.argtypes = [vp, vp, vp, i64, vp, i32, vp, vp, vp, vp, vp]
-        L.ibert_attention_decode_i8.argtypes = [vp, vp, vp, vp, vp, vp, i32, i32, i32, i64, i32, i32, i32, i32, i32, dbl, dbl, dbl,
+        L.ibert_attention_decode_i8.argtypes = [vp, vp, vp, vp, vp, vp, vp, i64, i32, i32, i32, i64, i32, i32, i32, i32, i32, dbl, dbl, dbl,
                                                 dbl, i32, vp, vp]
         L.ibert_attention_window_i8.argtypes = [vp, vp, vp, i32, i32, i64, i32, i32, i32, i32, dbl, dbl, dbl, dbl, i32, vp, vp]
         for name in ("ibert_attention_window_i8", "ibert_kv_slots", "ibert_rope_frequencies", "ibert_rope_rows", "ibert_qkv_rope_i8", "ibert_attention_decode_i8"):
@@ -571,17 +571,22 @@ class Context:
 
     def ibert_attention_decode_i8(self, q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, block_tables: torch.Tensor,
                                   lens: torch.Tensor, max_len: int, heads: int, S_q: float, S_k: float, S_v: float, S_ctx: float,
-                                  window: int = 0, sinks: int = 0, p_max: int = 255, out: torch.Tensor | None = None):
+                                  window: int = 0, sinks: int = 0, p_max: int = 255, out: torch.Tensor | None = None,
+                                  cu_seqlens: torch.Tensor | None = None):
         """Attention of one new token per sequence over the paged cache; ``q`` int8 [B, heads * 64], ``lens`` device int32 [B]
-        (the new token included), caches int8 [pages, kv_heads, page_size, 64]."""
+        (the new token included), caches int8 [pages, kv_heads, page_size, 64].  With ``cu_seqlens`` (device int32 [B + 1])
+        ``q`` has a row per new token and sequence b's is the last of its own; rows of other tokens are left as they were."""
         B, max_pages = block_tables.shape
         n_pages, kv_heads, page_size, D = k_cache.shape
-        assert D == 64 and v_cache.shape == k_cache.shape and q.numel() == B * heads * 64 and lens.numel() == B
+        rows = B if cu_seqlens is None else q.numel() // (heads * 64)
+        assert D == 64 and v_cache.shape == k_cache.shape and q.numel() == rows * heads * 64 and lens.numel() == B
+        assert cu_seqlens is None or cu_seqlens.numel() == B + 1
         if out is None:
-            out = q.new_empty((B, heads * 64))
+            out = q.new_empty((rows, heads * 64))
         assert out.numel() == q.numel()
         _chk(lib().ibert_attention_decode_i8(self.h, _dev(q, torch.int8), _dev(k_cache, torch.int8), _dev(v_cache, torch.int8),
-                                             _dev(block_tables, torch.int32), _dev(lens, torch.int32), B, max_len, max_pages, n_pages,
+                                             _dev(block_tables, torch.int32), _dev(lens, torch.int32), _dev(cu_seqlens, torch.int32), rows, B,
+                                             max_len, max_pages, n_pages,
                                              page_size, heads, kv_heads, window, sinks, S_q, S_k, S_v, S_ctx, p_max,
                                              _dev(out, torch.int8), None), "ibert_attention_decode_i8")
         return out, S_ctx

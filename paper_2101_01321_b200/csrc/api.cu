@@ -1206,7 +1206,8 @@ static int make_long_attn_consts(double S_q, double S_k, double S_v, double S_ct
 
 static int check_long_attention(int64_t max_len, int heads, int kv_heads, int window, int sinks) {
   if (window < 0 || sinks < 0) return IBERT_ERR_ARG;
-  if (heads < 1 || kv_heads < 1 || heads % kv_heads != 0 || heads > 4096 || max_len < 1) return IBERT_ERR_SHAPE;
+  if (heads < 1 || kv_heads < 1 || heads % kv_heads != 0 || heads > 4096 || max_len < 1 || max_len >= (int64_t(1) << 31) - 256)
+    return IBERT_ERR_SHAPE;
   if ((window > 0 ? std::min<int64_t>(max_len, (int64_t)window + sinks) : max_len) > kMaxVisible) return IBERT_ERR_SHAPE;
   return IBERT_OK;
 }
@@ -1232,27 +1233,30 @@ int ibert_attention_window_i8(ibert_ctx* ctx, const int8_t* qkv, const int32_t* 
 }
 
 int ibert_attention_decode_i8(ibert_ctx* ctx, const int8_t* q, const int8_t* k_cache, const int8_t* v_cache,
-                              const int32_t* block_tables, const int32_t* lens, int B, int max_len, int max_pages,
-                              int64_t n_pages, int page_size, int heads, int kv_heads, int window, int sinks, double S_q,
-                              double S_k, double S_v, double S_ctx, int p_max, int8_t* out, double* S_ret) {
+                              const int32_t* block_tables, const int32_t* lens, const int32_t* cu_seqlens, int64_t rows,
+                              int B, int max_len, int max_pages, int64_t n_pages, int page_size, int heads, int kv_heads,
+                              int window, int sinks, double S_q, double S_k, double S_v, double S_ctx, int p_max, int8_t* out,
+                              double* S_ret) {
   return guarded([&]() -> int {
   if (!ctx || B < 0) return IBERT_ERR_ARG;
   int rc = check_long_attention(max_len, heads, kv_heads, window, sinks);
   if (rc) return rc;
   const int log_page = log2_page(page_size);
   if (log_page < 0 || max_pages < 0 || max_len > (int64_t)max_pages << log_page || n_pages < 0 ||
-      n_pages >= (int64_t(1) << 31) >> log_page || (int64_t)B * heads >= (int64_t(1) << 24))
+      n_pages >= (int64_t(1) << 31) >> log_page || (int64_t)B * heads >= (int64_t(1) << 24) || rows < 0 ||
+      rows >= (int64_t(1) << 31) / heads || (!cu_seqlens && rows != B))
     return IBERT_ERR_SHAPE;
-  if (B > 0 && (!q || !k_cache || !v_cache || !block_tables || !lens || !out)) return IBERT_ERR_ARG;
-  if (!aligned16(q) || !aligned16(k_cache) || !aligned16(v_cache) || !aligned16(out) || !aligned4(block_tables) || !aligned4(lens))
+  if (B > 0 && rows > 0 && (!q || !k_cache || !v_cache || !block_tables || !lens || !out)) return IBERT_ERR_ARG;
+  if (!aligned16(q) || !aligned16(k_cache) || !aligned16(v_cache) || !aligned16(out) || !aligned4(block_tables) || !aligned4(lens) ||
+      !aligned4(cu_seqlens))
     return IBERT_ERR_ALIGN;
   LongAttnConsts k{};
   if ((rc = make_long_attn_consts(S_q, S_k, S_v, S_ctx, p_max, &k))) return rc;
   if (S_ret) *S_ret = S_ctx;
-  if (B == 0) return IBERT_OK;
+  if (B == 0 || rows == 0) return IBERT_OK;
   DeviceGuard guard(ctx->device);
   ProfileScope ps(ctx, IBERT_K_ATTENTION);
-  return launch_attention_decode(ctx, q, k_cache, v_cache, block_tables, lens, B, max_pages, (int)n_pages, log_page, max_len,
+  return launch_attention_decode(ctx, q, k_cache, v_cache, block_tables, lens, cu_seqlens, rows, B, max_pages, (int)n_pages, log_page, max_len,
                                  heads, kv_heads, window, sinks, k, out);
   });
 }

@@ -34,7 +34,8 @@ constexpr int kDecMaxSmem = 160 * 1024;
 
 struct DecodeArgs {
   const int8_t *q, *k_cache, *v_cache;
-  const int32_t *tables, *lens;
+  const int32_t *tables, *lens, *cu;     // cu: null, or [B + 1]: the row of sequence b is cu[b + 1] - 1
+  int64_t rows;
   int8_t* out;
   int32_t* status;
   int32_t heads, kv_heads, group, tiles_of_group;     // query heads per kv head, and in pieces of kMaxGroup
@@ -94,6 +95,13 @@ attention_decode_kernel(const __grid_constant__ DecodeArgs a) {
   int32_t len = ptx::ld_dep(a.lens + batch);
   bool bad = len < 0 || len > a.max_len;
   len = min(max(len, 0), a.max_len);
+  int64_t q_row = batch;                 // < 0: no new token, nothing to do
+  if (a.cu) {
+    const int32_t c0 = ptx::ld_dep(a.cu + batch), c1 = ptx::ld_dep(a.cu + batch + 1);
+    q_row = c1 > c0 ? c1 - 1 : -1;
+    if (q_row >= a.rows || (c1 > c0 && q_row < 0)) { bad = true; q_row = -1; }
+    if (q_row < 0) len = 0;
+  }
   const int start = a.window > 0 ? max(len - a.window, 0) : 0, first = min(a.sinks, start);
   const int tile_w = start / kTile, lead = min((first + kTile - 1) / kTile, tile_w);
   const int tiles = len > 0 ? lead + (len + kTile - 1) / kTile - tile_w : 0;
@@ -119,7 +127,7 @@ attention_decode_kernel(const __grid_constant__ DecodeArgs a) {
     s_place[i] = place;
   }
   uint4 q = make_uint4(0, 0, 0, 0);      // 16 bytes of head g, the A operand's rows 0 to 7 (rows 8 to 15 are zeros)
-  if (g < G) q = ptx::ld_dep(reinterpret_cast<const uint4*>(a.q + ((int64_t)batch * a.heads + head0 + g) * kHeadDim) + t);
+  if (g < G && q_row >= 0) q = ptx::ld_dep(reinterpret_cast<const uint4*>(a.q + (q_row * a.heads + head0 + g) * kHeadDim) + t);
   __syncthreads();                       // s_place, s_out and s_sum are filled
 
   // ---- a warp's stream of tiles, copied into a ring of its own: its keys, then its values (KEEP), or its keys, then a tile of
@@ -316,7 +324,7 @@ attention_decode_kernel(const __grid_constant__ DecodeArgs a) {
       o += ptx::ld_cluster_s32(ptx::map_to_cta(ptx::smem_addr(part), (uint32_t)c));
       total += (uint32_t)ptx::ld_cluster_s32(ptx::map_to_cta(ptx::smem_addr(&s_sum[h]), (uint32_t)c));
     }
-    a.out[((int64_t)batch * a.heads + head0 + h) * kHeadDim + d] = (int8_t)weighted_mean(o, row_share(total, k));
+    if (q_row >= 0) a.out[(q_row * a.heads + head0 + h) * kHeadDim + d] = (int8_t)weighted_mean(o, row_share(total, k));
   }
   if (bad) atomicCAS(a.status, 0, IBERT_ERR_VALUE_RANGE);
   if (cl > 1) ptx::cluster_sync();       // nobody leaves while a peer may still read its shared memory
@@ -325,11 +333,11 @@ attention_decode_kernel(const __grid_constant__ DecodeArgs a) {
 }  // namespace
 
 int launch_attention_decode(ibert_ctx* ctx, const int8_t* q, const int8_t* k_cache, const int8_t* v_cache,
-                            const int32_t* tables, const int32_t* lens, int B, int max_pages, int n_pages, int log_page,
+                            const int32_t* tables, const int32_t* lens, const int32_t* cu, int64_t rows, int B, int max_pages, int n_pages, int log_page,
                             int max_len, int heads, int kv_heads, int window, int sinks, const LongAttnConsts& k,
                             int8_t* out) {
   DecodeArgs a{};
-  a.q = q; a.k_cache = k_cache; a.v_cache = v_cache; a.tables = tables; a.lens = lens; a.out = out; a.status = ctx->d_status;
+  a.q = q; a.k_cache = k_cache; a.v_cache = v_cache; a.tables = tables; a.lens = lens; a.cu = cu; a.rows = rows; a.out = out; a.status = ctx->d_status;
   a.heads = heads; a.kv_heads = kv_heads; a.group = heads / kv_heads;
   a.tiles_of_group = (a.group + kMaxGroup - 1) / kMaxGroup;
   a.log_page = log_page; a.max_pages = max_pages; a.n_pages = n_pages; a.max_len = max_len; a.window = window; a.sinks = sinks;
@@ -340,11 +348,11 @@ int launch_attention_decode(ibert_ctx* ctx, const int8_t* q, const int8_t* k_cac
   if (window > 0) tiles = std::min<int64_t>(tiles, ((int64_t)window + kTile - 1) / kTile + 1 + ((int64_t)sinks + kTile - 1) / kTile);
   const bool keep = a.group <= 2;
   const int warps = keep ? 4 : 8, stages = keep ? 4 : 2;
-  const int rows = keep ? a.group : 0;
+  const int kept = keep ? a.group : 0;
   // (rings, scores, then the places of the tiles' halves)
   auto smem_of = [&](int c) {
     const int64_t n = (tiles + c - 1) / c;
-    return (int64_t)warps * stages * kTileBytes + rows * (n * kTile + 16) * 4 + n * 16;
+    return (int64_t)warps * stages * kTileBytes + kept * (n * kTile + 16) * 4 + n * 16;
   };
   int cl = 1;
   while (cl < kMaxCluster && items * cl < 2 * ctx->num_sms && (tiles + cl - 1) / cl > warps) cl <<= 1;

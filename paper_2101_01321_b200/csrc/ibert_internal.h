@@ -314,7 +314,7 @@ void make_short_quotient(LongAttnConsts* k);
 constexpr int kMaxVisible = 65536;       // visible keys per query: 255 * 128 * 65536 < 2^31
 
 int launch_attention_decode(ibert_ctx* ctx, const int8_t* q, const int8_t* k_cache, const int8_t* v_cache,
-                            const int32_t* tables, const int32_t* lens, int B, int max_pages, int n_pages, int log_page,
+                            const int32_t* tables, const int32_t* lens, const int32_t* cu, int64_t rows, int B, int max_pages, int n_pages, int log_page,
                             int max_len, int heads, int kv_heads, int window, int sinks, const LongAttnConsts& k,
                             int8_t* out);
 

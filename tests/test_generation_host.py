@@ -66,11 +66,12 @@ def test_qkv_rope_refuses(lib, kw, code):
 
 def test_no_tokens_are_no_work(lib):
     assert _rope(lib, T=0, qkv=None, out=None, positions=None) == 0
-    assert _decode(lib, B=0, q=None, out=None) == 0
+    assert _decode(lib, B=0, rows=0, q=None, out=None) == 0
+    assert _decode(lib, cu=P16, rows=0, q=None, out=None) == 0
 
 
 def _decode(lib, **kw):
-    a = dict(ctx=CTX, q=P16, k=P16, v=P16, tables=P16, lens=P16, B=2, max_len=100, max_pages=8, n_pages=16, page=16, heads=4,
+    a = dict(ctx=CTX, q=P16, k=P16, v=P16, tables=P16, lens=P16, cu=None, rows=2, B=2, max_len=100, max_pages=8, n_pages=16, page=16, heads=4,
              kv_heads=2, window=0, sinks=0, S_q=0.05, S_k=0.05, S_v=0.05, S_ctx=0.02, p_max=255, out=P16, S_ret=None) | kw
     return lib.ibert_attention_decode_i8(*a.values())
 
@@ -79,7 +80,9 @@ def _decode(lib, **kw):
     (dict(ctx=None), ARG), (dict(B=-1), ARG), (dict(window=-1), ARG), (dict(sinks=-1), ARG), (dict(p_max=100), ARG),
     (dict(max_len=0), SHAPE), (dict(max_len=129), SHAPE), (dict(heads=0), SHAPE), (dict(kv_heads=0), SHAPE), (dict(heads=3), SHAPE),
     (dict(page=40), SHAPE), (dict(n_pages=-1), SHAPE), (dict(n_pages=1 << 27), SHAPE), (dict(max_len=65537, max_pages=1 << 20), SHAPE),
-    (dict(max_len=80000, max_pages=1 << 20, window=65536, sinks=1), SHAPE), (dict(B=1 << 23), SHAPE),
+    (dict(max_len=80000, max_pages=1 << 20, window=65536, sinks=1), SHAPE), (dict(B=1 << 23, rows=1 << 23), SHAPE),
+    (dict(rows=3), SHAPE), (dict(cu=P16, rows=-1), SHAPE), (dict(cu=P16, rows=1 << 29), SHAPE), (dict(cu=P16 + 2), ALIGN), (dict(B=-1, rows=-1), ARG),
+    (dict(max_len=(1 << 31) - 256, max_pages=1 << 27, window=5), SHAPE),
     (dict(S_q=0.0), SCALE), (dict(S_ctx=float("inf")), SCALE), (dict(S_q=2.0, S_k=2.0), SCALE), (dict(S_q=1.5, S_k=1.4), SCALE),
     (dict(q=P16 + 8), ALIGN), (dict(k=P16 + 8), ALIGN), (dict(v=P16 + 8), ALIGN), (dict(out=P16 + 8), ALIGN), (dict(tables=P16 + 2), ALIGN),
     (dict(lens=P16 + 2), ALIGN)] + [({n: None}, ARG) for n in ("q", "k", "v", "tables", "lens", "out")])
@@ -96,7 +99,7 @@ def _window(lib, **kw):
 @pytest.mark.parametrize("kw,code", [
     (dict(ctx=None), ARG), (dict(B=-1), ARG), (dict(T=-1), ARG), (dict(window=-1), ARG), (dict(sinks=-1), ARG), (dict(p_max=1), ARG),
     (dict(qkv=None), ARG), (dict(cu=None), ARG), (dict(out=None), ARG), (dict(max_len=0), SHAPE), (dict(max_len=65537), SHAPE),
-    (dict(max_len=70000, window=65000, sinks=537), SHAPE), (dict(heads=0), SHAPE), (dict(heads=5), SHAPE), (dict(kv_heads=0), SHAPE),
+    (dict(max_len=70000, window=65000, sinks=537), SHAPE), (dict(max_len=(1 << 31) - 256, window=5), SHAPE), (dict(heads=0), SHAPE), (dict(heads=5), SHAPE), (dict(kv_heads=0), SHAPE),
     (dict(T=(1 << 31) - 256), SHAPE), (dict(S_k=0.0), SCALE), (dict(S_q=1.5, S_k=1.4), SCALE), (dict(S_v=float("nan")), SCALE),
     (dict(qkv=P16 + 8), ALIGN), (dict(out=P16 + 8), ALIGN), (dict(cu=P16 + 2), ALIGN)])
 def test_attention_window_refuses(lib, kw, code):

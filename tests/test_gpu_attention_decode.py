@@ -130,6 +130,38 @@ def test_bad_pages_and_lengths_are_reported_and_harmless():
         assert_same(host(out), ref.attention_decode(q, kc, vc, tables, taken, 0, 0, SC, 255))
 
 
+def test_rows_of_a_packed_step():
+    """Row offsets of a step in which some sequences get no token and others several: the last new token's row of each is
+    computed, all other rows stay; rows outside the tensor are left out."""
+    rng = np.random.default_rng(10)
+    new = np.array([1, 0, 3, 1, 0, 40, 1])
+    lens = np.array([50, 20, 33, 1, 0, 40, 700], np.int32)
+    cu = np.concatenate([[0], np.cumsum(new)]).astype(np.int32)
+    for heads, kv in ((4, 2), (6, 1)):
+        tables, kc, vc = _cache(rng, lens, kv, 16)
+        T = int(cu[-1]) + 4
+        q = rng.integers(-127, 128, (T, heads * 64)).astype(np.int8)
+        out = torch.full((T, heads * 64), 55, dtype=torch.int8, device="cuda")
+
+        def call(offsets):
+            out.fill_(55)
+            ctx().ibert_attention_decode_i8(dev(q), dev(kc), dev(vc), dev(tables), dev(lens), 700, heads, *SC, out=out, cu_seqlens=dev(offsets))
+            return host(out), ctx().ibert_last_status()
+
+        want = np.full((T, heads * 64), 55, np.int8)
+        has = np.flatnonzero(new)
+        want[cu[has + 1] - 1] = ref.attention_decode(q[cu[has + 1] - 1], kc, vc, tables[has], lens[has], 0, 0, SC, 255)
+        got, status = call(cu)
+        assert status == 0
+        assert_same(got, want)
+        bad = cu.copy()
+        bad[7] = T + 1                                               # the last sequence's row does not exist
+        want[cu[7] - 1] = 55
+        got, status = call(bad)
+        assert status == -8
+        assert_same(got, want)
+
+
 def test_many_calls_agree():
     rng = np.random.default_rng(8)
     tables, kc, vc = _cache(rng, [3000, 100], 1, 16)
