@@ -147,10 +147,6 @@ def _host(a, dtype) -> np.ndarray:
     return np.ascontiguousarray(a, dtype=dtype)
 
 
-def _np_ptr(a: np.ndarray | None) -> int:
-    return 0 if a is None else a.__array_interface__["data"][0]
-
-
 _ROPE_DESC = struct.Struct("6i2q3P4d")        # RopeDesc, packed at once (field by field it takes as long as the call)
 assert _ROPE_DESC.size == C.sizeof(RopeDesc)
 
@@ -211,6 +207,8 @@ class Context:
         sp = None if stream is None else stream.cuda_stream
         _chk(lib().ibert_create(C.byref(h), device, sp), "ibert_create")
         self.h = h
+        self._gammas = np.zeros((2, 64))     # ibert_qkv_rope_i8's, at addresses that are looked up once
+        self._gamma_ptrs = [self._gammas[i].ctypes.data for i in range(2)]
 
     def close(self):
         if self.h:
@@ -532,9 +530,13 @@ class Context:
         T = qkv.numel() // n
         dtype = qkv.dtype
         assert qkv.numel() == T * n and (dtype is torch.int8 or dtype is torch.int16)
-        gq = None if gamma_q is None else _host(gamma_q, np.float64)
-        gk = None if gamma_k is None else _host(gamma_k, np.float64)
-        assert (gq is None or gq.size == 64) and (gk is None or gk.size == 64)
+        gq = gk = 0
+        if gamma_q is not None:              # (read during the call)
+            assert len(gamma_q) == 64
+            self._gammas[0], gq = gamma_q, self._gamma_ptrs[0]
+        if gamma_k is not None:
+            assert len(gamma_k) == 64
+            self._gammas[1], gk = gamma_k, self._gamma_ptrs[1]
         max_pos = rot_dim = n_pages = page_size = 0
         if rope is not None:
             max_pos, rot_dim = rope.shape
@@ -548,7 +550,7 @@ class Context:
             out = torch.empty((T, cols), dtype=torch.int8, device=qkv.device)
         assert out.numel() == T * cols
         desc = _ROPE_DESC.pack(heads, kv_heads, 8 if dtype is torch.int8 else 16, rot_dim, int(interleaved), page_size, n_pages, max_pos,
-                               _dev(rope, torch.int16) or 0, _np_ptr(gq), _np_ptr(gk), S_in, S_q, S_k, S_v)
+                               _dev(rope, torch.int16) or 0, gq, gk, S_in, S_q, S_k, S_v)
         i32, i8 = torch.int32, torch.int8
         _chk(lib().ibert_qkv_rope_i8(self.h, desc, _dev(qkv, dtype), T, _dev(positions, i32), int(with_kv), _dev(out, i8),
                                      _dev(slots, i32), _dev(k_cache, i8), _dev(v_cache, i8), None), "ibert_qkv_rope_i8")

@@ -1200,7 +1200,6 @@ static int make_long_attn_consts(double S_q, double S_k, double S_v, double S_ct
   if (k->e.q_ln2 <= 2 || k->e.wide_post < 0) return IBERT_ERR_SCALE_RANGE;    // the unclamped quotient is not available
   const uint32_t top = (uint32_t)((int64_t)k->e.q_b * k->e.q_b + k->e.q_c) >> k->e.s_out;
   k->b_w = ((uint32_t)p_max << 24) / top;
-  make_short_quotient(k);
   return dyadic(S_v / S_ctx, &k->b, &k->c);
 }
 
@@ -1226,6 +1225,7 @@ int ibert_attention_window_i8(ibert_ctx* ctx, const int8_t* qkv, const int32_t* 
   if ((rc = make_long_attn_consts(S_q, S_k, S_v, S_ctx, p_max, &k))) return rc;
   if (S_ret) *S_ret = S_ctx;
   if (B == 0 || total_tokens == 0) return IBERT_OK;
+  make_short_quotient(&k);
   DeviceGuard guard(ctx->device);
   ProfileScope ps(ctx, IBERT_K_ATTENTION);
   return launch_attention_window(ctx, qkv, cu_seqlens, B, max_len, total_tokens, heads, kv_heads, window, sinks, k, out);
