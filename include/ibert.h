@@ -388,6 +388,17 @@ typedef struct ibert_rope_desc {
 int ibert_qkv_rope_i8(ibert_ctx* ctx, const ibert_rope_desc* desc, const void* qkv, int64_t T, const int32_t* positions,
                       int with_kv, int8_t* out, const int32_t* slots, int8_t* k_cache, int8_t* v_cache, double* S_ret);
 
+/* What the two attentions below have in common for every call of a model */
+typedef struct ibert_attention_desc {
+  int32_t heads, kv_heads;
+  int32_t max_len;            /* the longest sequence of a call */
+  int32_t window, sinks;      /* window 0: all keys up to the query; else the last `window` and the first `sinks` */
+  int32_t p_max;              /* 255 or 127 */
+  int32_t page_size, max_pages;  /* paged attention only, as n_pages */
+  int64_t n_pages;
+  double S_q, S_k, S_v, S_ctx;
+} ibert_attention_desc;
+
 /* Causal attention of packed prompts: qkv int8 [total_tokens][(heads + 2 kv_heads) 64], columns Q | K | V (what
    ibert_qkv_rope_i8 writes with with_kv = 1), sequence b in rows cu_seqlens[b] .. cu_seqlens[b+1] - 1 (device int32 [B+1],
    non-decreasing from 0, every length at most max_len); out int8 [total_tokens][heads 64] at S_ctx (*S_ret).  A query sees the
@@ -397,9 +408,8 @@ int ibert_qkv_rope_i8(ibert_ctx* ctx, const ibert_rope_desc* desc, const void* q
    At most 65536 visible keys: min(max_len, window + sinks if window > 0) <= 65536, else IBERT_ERR_SHAPE.  A sequence longer
    than max_len records IBERT_ERR_VALUE_RANGE in the context's status; its queries then see at most their last max_len keys.
    total_tokens < 2^31 - 256; scale and p_max errors as below. */
-int ibert_attention_window_i8(ibert_ctx* ctx, const int8_t* qkv, const int32_t* cu_seqlens, int B, int max_len,
-                              int64_t total_tokens, int heads, int kv_heads, int window, int sinks, double S_q, double S_k,
-                              double S_v, double S_ctx, int p_max, int8_t* out, double* S_ret);
+int ibert_attention_window_i8(ibert_ctx* ctx, const ibert_attention_desc* desc, const int8_t* qkv, const int32_t* cu_seqlens,
+                              int B, int64_t total_tokens, int8_t* out, double* S_ret);
 
 /* Attention of ONE new token per sequence over the paged cache, which already holds the token's own key and value:
    q int8 [rows][heads 64] at S_q, out int8 [rows][heads 64] at S_ctx (*S_ret).  cu_seqlens NULL: row b belongs to sequence
@@ -419,11 +429,9 @@ int ibert_attention_window_i8(ibert_ctx* ctx, const int8_t* qkv, const int32_t* 
    max_len <= max_pages * page_size, max_len < 2^31 - 256, rows * heads < 2^31.  A length above max_len (taken as max_len) or below 0, and a visible key on a page
    outside [0, n_pages) (the key is left out), record IBERT_ERR_VALUE_RANGE in the context's status.
    IBERT_ERR_SCALE_RANGE also for score scales so coarse that floor(ln2 / (S_q S_k / 8)) <= 2; p_max in {255, 127}. */
-int ibert_attention_decode_i8(ibert_ctx* ctx, const int8_t* q, const int8_t* k_cache, const int8_t* v_cache,
-                              const int32_t* block_tables, const int32_t* lens, const int32_t* cu_seqlens, int64_t rows,
-                              int B, int max_len, int max_pages, int64_t n_pages, int page_size, int heads, int kv_heads,
-                              int window, int sinks, double S_q, double S_k, double S_v, double S_ctx, int p_max, int8_t* out,
-                              double* S_ret);
+int ibert_attention_decode_i8(ibert_ctx* ctx, const ibert_attention_desc* desc, const int8_t* q, const int8_t* k_cache,
+                              const int8_t* v_cache, const int32_t* block_tables, const int32_t* lens, int B,
+                              const int32_t* cu_seqlens, int64_t rows, int8_t* out, double* S_ret);
 
 /* ---- h-GELU, the comparison function of the paper (Eq. 6; Table 1, Table 3) --------------------
    h-GELU(x) = x ReLU6(1.702 x + 3) / 6.  The paper notes that it can be computed with integers

@@ -46,6 +46,11 @@ class RopeDesc(C.Structure):
         (n, C.c_double) for n in ("S_in", "S_q", "S_k", "S_v")]
 
 
+class AttentionDesc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("heads", "kv_heads", "max_len", "window", "sinks", "p_max", "page_size", "max_pages")] + [
+        ("n_pages", C.c_int64)] + [(n, C.c_double) for n in ("S_q", "S_k", "S_v", "S_ctx")]
+
+
 def lib():
     """Loads the C-ABI library; fails loudly if it has not been built."""
     global _lib
@@ -114,9 +119,8 @@ def lib():
         L.ibert_rope_frequencies.argtypes = [i32, dbl, dbl, dbl, dbl, dbl, vp]
         L.ibert_rope_rows.argtypes = [vp, i32, i64, i64, dbl, vp]
         L.ibert_qkv_rope_i8.argtypes = [vp, vp, vp, i64, vp, i32, vp, vp, vp, vp, vp]
-        L.ibert_attention_decode_i8.argtypes = [vp, vp, vp, vp, vp, vp, vp, i64, i32, i32, i32, i64, i32, i32, i32, i32, i32, dbl, dbl, dbl,
-                                                dbl, i32, vp, vp]
-        L.ibert_attention_window_i8.argtypes = [vp, vp, vp, i32, i32, i64, i32, i32, i32, i32, dbl, dbl, dbl, dbl, i32, vp, vp]
+        L.ibert_attention_decode_i8.argtypes = [vp, vp, vp, vp, vp, vp, vp, i32, vp, i64, vp, vp]
+        L.ibert_attention_window_i8.argtypes = [vp, vp, vp, vp, i32, i64, vp, vp]
         for name in ("ibert_attention_window_i8", "ibert_kv_slots", "ibert_rope_frequencies", "ibert_rope_rows", "ibert_qkv_rope_i8", "ibert_attention_decode_i8"):
             getattr(L, name).restype = i32
         for name in ("ibert_create", "ibert_destroy", "ibert_last_status", "ibert_dyadic_from_double",
@@ -147,8 +151,10 @@ def _host(a, dtype) -> np.ndarray:
     return np.ascontiguousarray(a, dtype=dtype)
 
 
-_ROPE_DESC = struct.Struct("6i2q3P4d")        # RopeDesc, packed at once (field by field it takes as long as the call)
-assert _ROPE_DESC.size == C.sizeof(RopeDesc)
+# The descriptors packed at once (field by field that takes as long as the call)
+_ROPE_DESC = struct.Struct("6i2q3P4d")
+_ATTENTION_DESC = struct.Struct("8iq4d")
+assert _ROPE_DESC.size == C.sizeof(RopeDesc) and _ATTENTION_DESC.size == C.sizeof(AttentionDesc)
 
 
 def ibert_dyadic_from_double(m: float) -> tuple[int, int]:
@@ -566,9 +572,9 @@ class Context:
         if out is None:
             out = qkv.new_empty((T, heads * 64))
         assert out.numel() == T * heads * 64
-        _chk(lib().ibert_attention_window_i8(self.h, _dev(qkv, torch.int8), _dev(cu_seqlens, torch.int32), cu_seqlens.numel() - 1,
-                                             max_len, T, heads, kv_heads, window, sinks, S_q, S_k, S_v, S_ctx, p_max,
-                                             _dev(out, torch.int8), None), "ibert_attention_window_i8")
+        desc = _ATTENTION_DESC.pack(heads, kv_heads, max_len, window, sinks, p_max, 0, 0, 0, S_q, S_k, S_v, S_ctx)
+        _chk(lib().ibert_attention_window_i8(self.h, desc, _dev(qkv, torch.int8), _dev(cu_seqlens, torch.int32), cu_seqlens.numel() - 1,
+                                             T, _dev(out, torch.int8), None), "ibert_attention_window_i8")
         return out, S_ctx
 
     def ibert_attention_decode_i8(self, q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, block_tables: torch.Tensor,
@@ -586,11 +592,11 @@ class Context:
         if out is None:
             out = q.new_empty((rows, heads * 64))
         assert out.numel() == q.numel()
-        _chk(lib().ibert_attention_decode_i8(self.h, _dev(q, torch.int8), _dev(k_cache, torch.int8), _dev(v_cache, torch.int8),
-                                             _dev(block_tables, torch.int32), _dev(lens, torch.int32), _dev(cu_seqlens, torch.int32), rows, B,
-                                             max_len, max_pages, n_pages,
-                                             page_size, heads, kv_heads, window, sinks, S_q, S_k, S_v, S_ctx, p_max,
-                                             _dev(out, torch.int8), None), "ibert_attention_decode_i8")
+        i8, i32 = torch.int8, torch.int32
+        desc = _ATTENTION_DESC.pack(heads, kv_heads, max_len, window, sinks, p_max, page_size, max_pages, n_pages, S_q, S_k, S_v, S_ctx)
+        _chk(lib().ibert_attention_decode_i8(self.h, desc, _dev(q, i8), _dev(k_cache, i8), _dev(v_cache, i8), _dev(block_tables, i32),
+                                             _dev(lens, i32), B, _dev(cu_seqlens, i32), rows, _dev(out, i8), None),
+             "ibert_attention_decode_i8")
         return out, S_ctx
 
     # ------------------------------------------------------------------ encoder layer

@@ -1193,71 +1193,68 @@ int ibert_qkv_rope_i8(ibert_ctx* ctx, const ibert_rope_desc* d, const void* qkv,
   });
 }
 
-static int make_long_attn_consts(double S_q, double S_k, double S_v, double S_ctx, int p_max, LongAttnConsts* k) {
-  if (!good_scale(S_q) || !good_scale(S_k) || !good_scale(S_v) || !good_scale(S_ctx)) return IBERT_ERR_SCALE_RANGE;
-  int rc = make_exp_consts((S_q * S_k) / 8.0, p_max, &k->e);
+static int make_long_attn_consts(const ibert_attention_desc& d, LongAttnConsts* k) {
+  if (!good_scale(d.S_q) || !good_scale(d.S_k) || !good_scale(d.S_v) || !good_scale(d.S_ctx)) return IBERT_ERR_SCALE_RANGE;
+  int rc = make_exp_consts((d.S_q * d.S_k) / 8.0, d.p_max, &k->e);
   if (rc) return rc;
   if (k->e.q_ln2 <= 2 || k->e.wide_post < 0) return IBERT_ERR_SCALE_RANGE;    // the unclamped quotient is not available
   const uint32_t top = (uint32_t)((int64_t)k->e.q_b * k->e.q_b + k->e.q_c) >> k->e.s_out;
-  k->b_w = ((uint32_t)p_max << 24) / top;
-  return dyadic(S_v / S_ctx, &k->b, &k->c);
+  k->b_w = ((uint32_t)d.p_max << 24) / top;
+  return dyadic(d.S_v / d.S_ctx, &k->b, &k->c);
 }
 
-static int check_long_attention(int64_t max_len, int heads, int kv_heads, int window, int sinks) {
-  if (window < 0 || sinks < 0) return IBERT_ERR_ARG;
-  if (heads < 1 || kv_heads < 1 || heads % kv_heads != 0 || heads > 4096 || max_len < 1 || max_len >= (int64_t(1) << 31) - 256)
+static int check_long_attention(const ibert_attention_desc& d) {
+  if (d.window < 0 || d.sinks < 0) return IBERT_ERR_ARG;
+  if (d.heads < 1 || d.kv_heads < 1 || d.heads % d.kv_heads != 0 || d.heads > 4096 || d.max_len < 1 || d.max_len >= INT32_MAX - 255)
     return IBERT_ERR_SHAPE;
-  if ((window > 0 ? std::min<int64_t>(max_len, (int64_t)window + sinks) : max_len) > kMaxVisible) return IBERT_ERR_SHAPE;
+  if ((d.window > 0 ? std::min<int64_t>(d.max_len, (int64_t)d.window + d.sinks) : d.max_len) > kMaxVisible) return IBERT_ERR_SHAPE;
   return IBERT_OK;
 }
 
-int ibert_attention_window_i8(ibert_ctx* ctx, const int8_t* qkv, const int32_t* cu_seqlens, int B, int max_len,
-                              int64_t total_tokens, int heads, int kv_heads, int window, int sinks, double S_q, double S_k,
-                              double S_v, double S_ctx, int p_max, int8_t* out, double* S_ret) {
+int ibert_attention_window_i8(ibert_ctx* ctx, const ibert_attention_desc* d, const int8_t* qkv, const int32_t* cu_seqlens,
+                              int B, int64_t total_tokens, int8_t* out, double* S_ret) {
   return guarded([&]() -> int {
-  if (!ctx || B < 0 || total_tokens < 0) return IBERT_ERR_ARG;
-  int rc = check_long_attention(max_len, heads, kv_heads, window, sinks);
+  if (!ctx || !d || B < 0 || total_tokens < 0) return IBERT_ERR_ARG;
+  int rc = check_long_attention(*d);
   if (rc) return rc;
   if (total_tokens >= (int64_t(1) << 31) - 256 || B >= 1 << 30) return IBERT_ERR_SHAPE;
   if (B > 0 && total_tokens > 0 && (!qkv || !cu_seqlens || !out)) return IBERT_ERR_ARG;
   if (!aligned16(qkv) || !aligned16(out) || !aligned4(cu_seqlens)) return IBERT_ERR_ALIGN;
   LongAttnConsts k{};
-  if ((rc = make_long_attn_consts(S_q, S_k, S_v, S_ctx, p_max, &k))) return rc;
-  if (S_ret) *S_ret = S_ctx;
+  if ((rc = make_long_attn_consts(*d, &k))) return rc;
+  if (S_ret) *S_ret = d->S_ctx;
   if (B == 0 || total_tokens == 0) return IBERT_OK;
   make_short_quotient(&k);
   DeviceGuard guard(ctx->device);
   ProfileScope ps(ctx, IBERT_K_ATTENTION);
-  return launch_attention_window(ctx, qkv, cu_seqlens, B, max_len, total_tokens, heads, kv_heads, window, sinks, k, out);
+  return launch_attention_window(ctx, qkv, cu_seqlens, B, d->max_len, total_tokens, d->heads, d->kv_heads, d->window, d->sinks, k, out);
   });
 }
 
-int ibert_attention_decode_i8(ibert_ctx* ctx, const int8_t* q, const int8_t* k_cache, const int8_t* v_cache,
-                              const int32_t* block_tables, const int32_t* lens, const int32_t* cu_seqlens, int64_t rows,
-                              int B, int max_len, int max_pages, int64_t n_pages, int page_size, int heads, int kv_heads,
-                              int window, int sinks, double S_q, double S_k, double S_v, double S_ctx, int p_max, int8_t* out,
-                              double* S_ret) {
+int ibert_attention_decode_i8(ibert_ctx* ctx, const ibert_attention_desc* d, const int8_t* q, const int8_t* k_cache,
+                              const int8_t* v_cache, const int32_t* block_tables, const int32_t* lens, int B,
+                              const int32_t* cu_seqlens, int64_t rows, int8_t* out, double* S_ret) {
   return guarded([&]() -> int {
-  if (!ctx || B < 0) return IBERT_ERR_ARG;
-  int rc = check_long_attention(max_len, heads, kv_heads, window, sinks);
+  if (!ctx || !d || B < 0) return IBERT_ERR_ARG;
+  int rc = check_long_attention(*d);
   if (rc) return rc;
-  const int log_page = log2_page(page_size);
-  if (log_page < 0 || max_pages < 0 || max_len > (int64_t)max_pages << log_page || n_pages < 0 ||
-      n_pages >= (int64_t(1) << 31) >> log_page || (int64_t)B * heads >= (int64_t(1) << 24) || rows < 0 ||
-      rows >= (int64_t(1) << 31) / heads || (!cu_seqlens && rows != B))
+  const int log_page = log2_page(d->page_size);
+  if (log_page < 0 || d->max_pages < 0 || d->max_len > (int64_t)d->max_pages << log_page || d->n_pages < 0 ||
+      d->n_pages >= (int64_t(1) << 31) >> log_page || (int64_t)B * d->heads >= (int64_t(1) << 24) || rows < 0 ||
+      rows >= (int64_t(1) << 31) / d->heads || (!cu_seqlens && rows != B))
     return IBERT_ERR_SHAPE;
   if (B > 0 && rows > 0 && (!q || !k_cache || !v_cache || !block_tables || !lens || !out)) return IBERT_ERR_ARG;
   if (!aligned16(q) || !aligned16(k_cache) || !aligned16(v_cache) || !aligned16(out) || !aligned4(block_tables) || !aligned4(lens) ||
       !aligned4(cu_seqlens))
     return IBERT_ERR_ALIGN;
   LongAttnConsts k{};
-  if ((rc = make_long_attn_consts(S_q, S_k, S_v, S_ctx, p_max, &k))) return rc;
-  if (S_ret) *S_ret = S_ctx;
+  if ((rc = make_long_attn_consts(*d, &k))) return rc;
+  if (S_ret) *S_ret = d->S_ctx;
   if (B == 0 || rows == 0) return IBERT_OK;
   DeviceGuard guard(ctx->device);
   ProfileScope ps(ctx, IBERT_K_ATTENTION);
-  return launch_attention_decode(ctx, q, k_cache, v_cache, block_tables, lens, cu_seqlens, rows, B, max_pages, (int)n_pages, log_page, max_len,
-                                 heads, kv_heads, window, sinks, k, out);
+  return launch_attention_decode(ctx, q, k_cache, v_cache, block_tables, lens, cu_seqlens, rows, B, d->max_pages, (int)d->n_pages,
+                                 log_page, d->max_len, d->heads, d->kv_heads, d->window, d->sinks, k, out);
   });
 }
 

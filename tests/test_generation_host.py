@@ -70,16 +70,25 @@ def test_no_tokens_are_no_work(lib):
     assert _decode(lib, cu=P16, rows=0, q=None, out=None) == 0
 
 
+def _desc(kw):
+    """The fields of ibert_attention_desc out of kw, and the rest."""
+    from paper_2101_01321_b200.binding import AttentionDesc
+    names = [n for n, _ in AttentionDesc._fields_]
+    f = dict(heads=4, kv_heads=2, max_len=100, window=0, sinks=0, p_max=255, page_size=16, max_pages=8, n_pages=16, S_q=0.05, S_k=0.05,
+             S_v=0.05, S_ctx=0.02) | {n: x for n, x in kw.items() if n in names}
+    return C.byref(AttentionDesc(*(f[n] for n in names))), {n: x for n, x in kw.items() if n not in names}
+
+
 def _decode(lib, **kw):
-    a = dict(ctx=CTX, q=P16, k=P16, v=P16, tables=P16, lens=P16, cu=None, rows=2, B=2, max_len=100, max_pages=8, n_pages=16, page=16, heads=4,
-             kv_heads=2, window=0, sinks=0, S_q=0.05, S_k=0.05, S_v=0.05, S_ctx=0.02, p_max=255, out=P16, S_ret=None) | kw
+    desc, kw = _desc(kw)
+    a = dict(ctx=CTX, desc=desc, q=P16, k=P16, v=P16, tables=P16, lens=P16, B=2, cu=None, rows=2, out=P16, S_ret=None) | kw
     return lib.ibert_attention_decode_i8(*a.values())
 
 
 @pytest.mark.parametrize("kw,code", [
     (dict(ctx=None), ARG), (dict(B=-1), ARG), (dict(window=-1), ARG), (dict(sinks=-1), ARG), (dict(p_max=100), ARG),
     (dict(max_len=0), SHAPE), (dict(max_len=129), SHAPE), (dict(heads=0), SHAPE), (dict(kv_heads=0), SHAPE), (dict(heads=3), SHAPE),
-    (dict(page=40), SHAPE), (dict(n_pages=-1), SHAPE), (dict(n_pages=1 << 27), SHAPE), (dict(max_len=65537, max_pages=1 << 20), SHAPE),
+    (dict(page_size=40), SHAPE), (dict(desc=None), ARG), (dict(n_pages=-1), SHAPE), (dict(n_pages=1 << 27), SHAPE), (dict(max_len=65537, max_pages=1 << 20), SHAPE),
     (dict(max_len=80000, max_pages=1 << 20, window=65536, sinks=1), SHAPE), (dict(B=1 << 23, rows=1 << 23), SHAPE),
     (dict(rows=3), SHAPE), (dict(cu=P16, rows=-1), SHAPE), (dict(cu=P16, rows=1 << 29), SHAPE), (dict(cu=P16 + 2), ALIGN), (dict(B=-1, rows=-1), ARG),
     (dict(max_len=(1 << 31) - 256, max_pages=1 << 27, window=5), SHAPE),
@@ -91,8 +100,8 @@ def test_attention_decode_refuses(lib, kw, code):
 
 
 def _window(lib, **kw):
-    a = dict(ctx=CTX, qkv=P16, cu=P16, B=2, max_len=100, T=50, heads=4, kv_heads=2, window=0, sinks=0, S_q=0.05, S_k=0.05, S_v=0.05,
-             S_ctx=0.02, p_max=255, out=P16, S_ret=None) | kw
+    desc, kw = _desc(kw)
+    a = dict(ctx=CTX, desc=desc, qkv=P16, cu=P16, B=2, T=50, out=P16, S_ret=None) | kw
     return lib.ibert_attention_window_i8(*a.values())
 
 
