@@ -333,7 +333,7 @@ int ibert_classifier_packed_i8(ibert_ctx* ctx, const int8_t* x, const int32_t* c
        positions[i] = lens[b] + j and slots[i] its slot; entries from cu_seqlens[B] to max_tokens - 1 get slot -1 and
        position 0 (ibert_qkv_rope_i8 stores nothing for slot -1);
      - lens_out[b] = lens[b] + new_lens[b] (0: ended) and *n_free_out are the lengths and the stack after the step.
-   lens_out may be lens and n_free_out may be n_free; no other arrays may overlap.  New tokens past max_tokens in the
+   lens_out may be lens and n_free_out may be n_free; no other arrays may overlap (IBERT_ERR_ARG where two start at one address).  New tokens past max_tokens in the
    running count are left out.  A token without a page (the stack is empty, or the request's table full) gets slot -1, its
    page's entry -1, and does not count in lens_out.  Both record IBERT_ERR_VALUE_RANGE in the context's status, as do lengths
    outside [0, max_pages * page_size] and an *n_free outside [0, free_capacity] (taken as the nearest bound).
@@ -406,7 +406,8 @@ typedef struct ibert_attention_desc {
    first `sinks` of the sequence.  Rows from cu_seqlens[B] on are left as they were.  Weights and result as defined for
    ibert_attention_decode_i8 below -- a token's context is the same bit for bit whichever of the two computes it.
    At most 65536 visible keys: min(max_len, window + sinks if window > 0) <= 65536, else IBERT_ERR_SHAPE.  A sequence longer
-   than max_len records IBERT_ERR_VALUE_RANGE in the context's status; its queries then see at most their last max_len keys.
+   than max_len, or one that reaches past total_tokens, records IBERT_ERR_VALUE_RANGE in the context's status; queries then see at
+   most their last max_len keys.  out must not overlap qkv.
    total_tokens < 2^31 - 256; scale and p_max errors as below. */
 int ibert_attention_window_i8(ibert_ctx* ctx, const ibert_attention_desc* desc, const int8_t* qkv, const int32_t* cu_seqlens,
                               int B, int64_t total_tokens, int8_t* out, double* S_ret);
@@ -428,7 +429,7 @@ int ibert_attention_window_i8(ibert_ctx* ctx, const ibert_attention_desc* desc, 
    At most 65536 visible keys: min(max_len, window + sinks if window > 0) <= 65536, else IBERT_ERR_SHAPE; window, sinks >= 0;
    max_len <= max_pages * page_size, max_len < 2^31 - 256, rows * heads < 2^31.  A length above max_len (taken as max_len) or below 0, and a visible key on a page
    outside [0, n_pages) (the key is left out), record IBERT_ERR_VALUE_RANGE in the context's status.
-   IBERT_ERR_SCALE_RANGE also for score scales so coarse that floor(ln2 / (S_q S_k / 8)) <= 2; p_max in {255, 127}. */
+   out must not overlap the other arrays.  IBERT_ERR_SCALE_RANGE also for score scales so coarse that floor(ln2 / (S_q S_k / 8)) <= 2; p_max in {255, 127}. */
 int ibert_attention_decode_i8(ibert_ctx* ctx, const ibert_attention_desc* desc, const int8_t* q, const int8_t* k_cache,
                               const int8_t* v_cache, const int32_t* block_tables, const int32_t* lens, int B,
                               const int32_t* cu_seqlens, int64_t rows, int8_t* out, double* S_ret);

@@ -1103,6 +1103,13 @@ int ibert_kv_slots(ibert_ctx* ctx, const int32_t* lens, const int32_t* new_lens,
   if (!n_free || !n_free_out || !cu_seqlens || (free_capacity > 0 && !free_pages) || (max_tokens > 0 && (!slots || !positions)) ||
       (B > 0 && (!lens || !new_lens || !lens_out || (max_pages > 0 && !block_tables))))
     return IBERT_ERR_ARG;
+  const void* const written[] = {lens_out, n_free_out, cu_seqlens, slots, positions, block_tables, free_pages};
+  for (const void* a : written) {
+    if (!a) continue;
+    int same = 0;
+    for (const void* b : written) same += a == b;
+    if (same > 1 || a == new_lens || (a == lens && a != lens_out) || (a == n_free && a != n_free_out)) return IBERT_ERR_ARG;
+  }
   for (const void* p : {(const void*)lens, (const void*)new_lens, (const void*)block_tables, (const void*)free_pages,
                         (const void*)n_free, (const void*)lens_out, (const void*)n_free_out, (const void*)cu_seqlens,
                         (const void*)slots, (const void*)positions})
@@ -1168,7 +1175,7 @@ int ibert_qkv_rope_i8(ibert_ctx* ctx, const ibert_rope_desc* d, const void* qkv,
     a.n_slots = d->n_pages << a.log_page;
   }
   if (d->rot_dim > 0 && (d->max_pos < 1 || !d->rope || (T > 0 && !positions))) return IBERT_ERR_ARG;
-  if (T > 0 && (!qkv || !out)) return IBERT_ERR_ARG;
+  if (T > 0 && (!qkv || !out || out == qkv || out == k_cache || out == v_cache || (k_cache && k_cache == v_cache))) return IBERT_ERR_ARG;
   if (!aligned16(qkv) || !aligned16(out) || !aligned16(k_cache) || !aligned16(v_cache) || !aligned4(slots) ||
       (d->rot_dim > 0 && (!aligned16(d->rope) || !aligned4(positions))))
     return IBERT_ERR_ALIGN;
@@ -1218,7 +1225,7 @@ int ibert_attention_window_i8(ibert_ctx* ctx, const ibert_attention_desc* d, con
   int rc = check_long_attention(*d);
   if (rc) return rc;
   if (total_tokens >= (int64_t(1) << 31) - 256 || B >= 1 << 30) return IBERT_ERR_SHAPE;
-  if (B > 0 && total_tokens > 0 && (!qkv || !cu_seqlens || !out)) return IBERT_ERR_ARG;
+  if (B > 0 && total_tokens > 0 && (!qkv || !cu_seqlens || !out || out == qkv)) return IBERT_ERR_ARG;
   if (!aligned16(qkv) || !aligned16(out) || !aligned4(cu_seqlens)) return IBERT_ERR_ALIGN;
   LongAttnConsts k{};
   if ((rc = make_long_attn_consts(*d, &k))) return rc;
@@ -1243,7 +1250,8 @@ int ibert_attention_decode_i8(ibert_ctx* ctx, const ibert_attention_desc* d, con
       d->n_pages >= (int64_t(1) << 31) >> log_page || (int64_t)B * d->heads >= (int64_t(1) << 24) || rows < 0 ||
       rows >= (int64_t(1) << 31) / d->heads || (!cu_seqlens && rows != B))
     return IBERT_ERR_SHAPE;
-  if (B > 0 && rows > 0 && (!q || !k_cache || !v_cache || !block_tables || !lens || !out)) return IBERT_ERR_ARG;
+  if (B > 0 && rows > 0 && (!q || !k_cache || !v_cache || !block_tables || !lens || !out || out == q || out == k_cache || out == v_cache))
+    return IBERT_ERR_ARG;
   if (!aligned16(q) || !aligned16(k_cache) || !aligned16(v_cache) || !aligned16(out) || !aligned4(block_tables) || !aligned4(lens) ||
       !aligned4(cu_seqlens))
     return IBERT_ERR_ALIGN;

@@ -16,13 +16,14 @@ def lib():
 
 # A context that is never looked into: every call below is refused before that
 CTX = C.create_string_buffer(1 << 16)
-MEM = C.create_string_buffer(1 << 12)
+MEM = C.create_string_buffer(1 << 13)
 P16 = (C.addressof(MEM) + 255) // 256 * 256
+P = [P16 + 256 * i for i in range(8)]          # arrays that start at addresses of their own
 
 
 def _slots(lib, **kw):
-    a = dict(ctx=CTX, lens=P16, new=P16, tables=P16, B=4, max_pages=8, page=16, free=P16, cap=64, n_free=P16, max_tokens=16,
-             lens_out=P16, n_out=P16, cu=P16, slots=P16, positions=P16) | kw
+    a = dict(ctx=CTX, lens=P[0], new=P[1], tables=P[2], B=4, max_pages=8, page=16, free=P[3], cap=64, n_free=P[4], max_tokens=16,
+             lens_out=P[0], n_out=P[4], cu=P[5], slots=P[6], positions=P[7]) | kw
     return lib.ibert_kv_slots(*a.values())
 
 
@@ -31,13 +32,14 @@ def _slots(lib, **kw):
     (dict(page=0), SHAPE), (dict(page=8), SHAPE), (dict(page=24), SHAPE), (dict(page=512), SHAPE), (dict(B=8193), SHAPE),
     (dict(max_pages=1 << 27), SHAPE), (dict(max_pages=1 << 22, B=1024), SHAPE), (dict(max_tokens=1 << 31), SHAPE),
     (dict(cap=1 << 31), SHAPE)] + [
+    (dict(lens_out=P[1]), ARG), (dict(slots=P[7]), ARG), (dict(cu=P[0]), ARG), (dict(positions=P[4]), ARG), (dict(free=P[2]), ARG)] + [
     ({n: None}, ARG) for n in ("lens", "new", "tables", "free", "n_free", "lens_out", "n_out", "cu", "slots", "positions")] + [
     ({n: P16 + 2}, ALIGN) for n in ("lens", "new", "tables", "free", "n_free", "lens_out", "n_out", "cu", "slots", "positions")])
 def test_kv_slots_refuses(lib, kw, code):
     assert _slots(lib, **kw) == code
 
 
-def _rope(lib, ctx=CTX, qkv=P16, T=4, positions=P16, with_kv=1, out=P16, slots=None, k=None, v=None, **kw):
+def _rope(lib, ctx=CTX, qkv=P16, T=4, positions=P16, with_kv=1, out=P[1], slots=None, k=None, v=None, **kw):
     from paper_2101_01321_b200.binding import RopeDesc
     gamma = np.ones(64)
     d = RopeDesc(4, 2, 8, 64, 0, 16, 8, 100, P16, None, None, 0.03, 0.03, 0.03, 0.03)
@@ -46,13 +48,14 @@ def _rope(lib, ctx=CTX, qkv=P16, T=4, positions=P16, with_kv=1, out=P16, slots=N
     return lib.ibert_qkv_rope_i8(ctx, C.byref(d), qkv, T, positions, with_kv, out, slots, k, v, None)
 
 
-CACHE = dict(slots=P16, k=P16, v=P16)
+CACHE = dict(slots=P16, k=P[2], v=P[3])
 
 
 @pytest.mark.parametrize("kw,code", [
     (dict(ctx=None), ARG), (dict(T=-1), ARG), (dict(with_kv=2), ARG), (dict(interleaved=2), ARG), (dict(qkv=None), ARG),
     (dict(out=None), ARG), (dict(positions=None), ARG), (dict(rope=None), ARG), (dict(max_pos=0), ARG), (dict(gamma_q="ones"), ARG),
-    (dict(gamma_k="ones"), ARG), (dict(slots=P16), ARG), (dict(k=P16, v=P16), ARG), (dict(slots=P16, k=P16), ARG),
+    (dict(gamma_k="ones"), ARG), (dict(slots=P16), ARG), (dict(k=P[2], v=P[3]), ARG), (dict(slots=P16, k=P[2]), ARG), (dict(out=P16), ARG),
+    (dict(CACHE, v=P[2]), ARG), (dict(CACHE, k=P[1]), ARG),
     (dict(heads=0), SHAPE), (dict(kv_heads=0), SHAPE), (dict(kv_heads=3), SHAPE), (dict(in_bits=32), SHAPE), (dict(rot_dim=4), SHAPE),
     (dict(rot_dim=72), SHAPE), (dict(rot_dim=-8), SHAPE), (dict(heads=4098), SHAPE), (dict(T=1 << 31), SHAPE),
     (dict(CACHE, page_size=48), SHAPE), (dict(CACHE, n_pages=-1), SHAPE), (dict(CACHE, n_pages=1 << 27), SHAPE),
@@ -81,7 +84,7 @@ def _desc(kw):
 
 def _decode(lib, **kw):
     desc, kw = _desc(kw)
-    a = dict(ctx=CTX, desc=desc, q=P16, k=P16, v=P16, tables=P16, lens=P16, B=2, cu=None, rows=2, out=P16, S_ret=None) | kw
+    a = dict(ctx=CTX, desc=desc, q=P16, k=P[1], v=P[2], tables=P16, lens=P16, B=2, cu=None, rows=2, out=P[3], S_ret=None) | kw
     return lib.ibert_attention_decode_i8(*a.values())
 
 
@@ -90,7 +93,7 @@ def _decode(lib, **kw):
     (dict(max_len=0), SHAPE), (dict(max_len=129), SHAPE), (dict(heads=0), SHAPE), (dict(kv_heads=0), SHAPE), (dict(heads=3), SHAPE),
     (dict(page_size=40), SHAPE), (dict(desc=None), ARG), (dict(n_pages=-1), SHAPE), (dict(n_pages=1 << 27), SHAPE), (dict(max_len=65537, max_pages=1 << 20), SHAPE),
     (dict(max_len=80000, max_pages=1 << 20, window=65536, sinks=1), SHAPE), (dict(B=1 << 23, rows=1 << 23), SHAPE),
-    (dict(rows=3), SHAPE), (dict(cu=P16, rows=-1), SHAPE), (dict(cu=P16, rows=1 << 29), SHAPE), (dict(cu=P16 + 2), ALIGN), (dict(B=-1, rows=-1), ARG),
+    (dict(out=P16), ARG), (dict(out=P[1]), ARG), (dict(rows=3), SHAPE), (dict(cu=P16, rows=-1), SHAPE), (dict(cu=P16, rows=1 << 29), SHAPE), (dict(cu=P16 + 2), ALIGN), (dict(B=-1, rows=-1), ARG),
     (dict(max_len=(1 << 31) - 256, max_pages=1 << 27, window=5), SHAPE),
     (dict(S_q=0.0), SCALE), (dict(S_ctx=float("inf")), SCALE), (dict(S_q=2.0, S_k=2.0), SCALE), (dict(S_q=1.5, S_k=1.4), SCALE),
     (dict(q=P16 + 8), ALIGN), (dict(k=P16 + 8), ALIGN), (dict(v=P16 + 8), ALIGN), (dict(out=P16 + 8), ALIGN), (dict(tables=P16 + 2), ALIGN),
@@ -101,13 +104,13 @@ def test_attention_decode_refuses(lib, kw, code):
 
 def _window(lib, **kw):
     desc, kw = _desc(kw)
-    a = dict(ctx=CTX, desc=desc, qkv=P16, cu=P16, B=2, T=50, out=P16, S_ret=None) | kw
+    a = dict(ctx=CTX, desc=desc, qkv=P16, cu=P16, B=2, T=50, out=P[1], S_ret=None) | kw
     return lib.ibert_attention_window_i8(*a.values())
 
 
 @pytest.mark.parametrize("kw,code", [
     (dict(ctx=None), ARG), (dict(B=-1), ARG), (dict(T=-1), ARG), (dict(window=-1), ARG), (dict(sinks=-1), ARG), (dict(p_max=1), ARG),
-    (dict(qkv=None), ARG), (dict(cu=None), ARG), (dict(out=None), ARG), (dict(max_len=0), SHAPE), (dict(max_len=65537), SHAPE),
+    (dict(qkv=None), ARG), (dict(cu=None), ARG), (dict(out=None), ARG), (dict(out=P16), ARG), (dict(max_len=0), SHAPE), (dict(max_len=65537), SHAPE),
     (dict(max_len=70000, window=65000, sinks=537), SHAPE), (dict(max_len=(1 << 31) - 256, window=5), SHAPE), (dict(heads=0), SHAPE), (dict(heads=5), SHAPE), (dict(kv_heads=0), SHAPE),
     (dict(T=(1 << 31) - 256), SHAPE), (dict(S_k=0.0), SCALE), (dict(S_q=1.5, S_k=1.4), SCALE), (dict(S_v=float("nan")), SCALE),
     (dict(qkv=P16 + 8), ALIGN), (dict(out=P16 + 8), ALIGN), (dict(cu=P16 + 2), ALIGN)])

@@ -95,6 +95,36 @@ def test_many_sequences_of_random_lengths():
         _run(rng, lens, 2, 2, 17, 2, max_len=top)
 
 
+@pytest.mark.parametrize("scales", [(0.05, 0.04, 0.03, 0.01), (0.02, 0.02, 0.1, 0.1), (0.003, 0.003, 0.1, 0.1), (1e-4, 1e-4, 1.0, 1.0)])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (70, 3)])
+def test_more_ctas_than_the_gpu_holds(scales, window, sinks):
+    """600 CTAs: one thread per row, every form of the exponential."""
+    _run(np.random.default_rng(9), [300, 1, 250, 64, 0, 365, 200], 60, 4, window, sinks, scales=scales)
+
+
+def test_sequences_past_the_tensor_are_reported():
+    rng = np.random.default_rng(11)
+    qkv = rng.integers(-127, 128, (100, 3 * 64)).astype(np.int8)
+    out, _ = ctx().ibert_attention_window_i8(dev(qkv), dev(np.array([0, 60, 130], np.int32)), 130, 1, 1, *SC)
+    assert ctx().ibert_last_status() == -8
+    assert_same(host(out), ref.attention_window(qkv, np.array([0, 60, 100]), 1, 1, 0, 0, SC, 255))
+
+
+def test_tensors_past_2_gib():
+    """Row offsets past 2^31 elements: the last rows of a packed tensor of 2.2e9 bytes."""
+    T, heads, kv = 700001, 40, 5
+    qkv = torch.randint(-100, 101, (T, (heads + 2 * kv) * 64), dtype=torch.int8, device="cuda")
+    lens = np.full(T // 70, 70)
+    cu = np.concatenate([[0], np.cumsum(lens), [T]]).astype(np.int32)
+    out, _ = ctx().ibert_attention_window_i8(qkv, dev(cu), 100, heads, kv, *SC, window=20, sinks=2)
+    ctx().check()
+    for b in (0, 5000, len(cu) - 3, len(cu) - 2):
+        rows = slice(int(cu[b]), int(cu[b + 1]))
+        n = rows.stop - rows.start
+        want = ref.attention_window(host(qkv[rows]), np.array([0, n]), heads, kv, 20, 2, SC, 255)
+        assert_same(host(out[rows]), want, f"sequence {b}")
+
+
 def test_near_the_first_operator_of_its_kind():
     """One sequence, its last query: the weighted mean against ibert_attention_i8's divide-first form on the same keys.  There
     every probability is floored to a 255th, so L keys lose up to L/255 of their weight; here each weight is rounded to half

@@ -107,6 +107,31 @@ def test_scales(S_q):
         _run(x, S_in, 2, 1, norm, rope, np.arange(9, dtype=np.int32), True, True, False, sc=sc)
 
 
+def test_multipliers_far_above_one():
+    """Without a norm, scales of the result so fine that almost everything is clamped (shifts below 17)."""
+    rng = np.random.default_rng(12)
+    for bits in (8, 16):
+        x, S_in = _x(rng, 9, 4, bits)
+        x[0] = 0
+        x[1, ::2] = 1
+        _run(x, S_in, 2, 1, (None, None), None, None, False, True, False, sc=dict(S_q=1e-7, S_k=3e-8, S_v=1e-6))
+
+
+def test_tensors_past_2_gib():
+    T, heads, kv = 700001, 40, 5
+    n = (heads + 2 * kv) * 64
+    qkv = torch.randint(-100, 101, (T, n), dtype=torch.int8, device="cuda")
+    rng = np.random.default_rng(13)
+    gq, gk = _gammas(rng)
+    rope = binding.ibert_rope_rows(binding.ibert_rope_frequencies(64), 100)
+    pos = (np.arange(T) % 100).astype(np.int32)
+    out, _ = ctx().ibert_qkv_rope_i8(qkv, 0.01, heads, kv, *SC.values(), gq, gk, rope=dev(rope), positions=dev(pos))
+    ctx().check()
+    for rows in (slice(0, 3), slice(699040, 699060), slice(T - 5, T)):
+        q, k, v = ref.qkv_rope(host(qkv[rows]), heads, kv, 0.01, *SC.values(), gq, gk, rope, pos[rows], False)
+        assert_same(host(out[rows]), np.concatenate([q, k, v], 1).reshape(-1, n))
+
+
 def test_long_positions_and_stretched_frequencies():
     rng = np.random.default_rng(2)
     f = binding.ibert_rope_frequencies(64, 500000.0, 8.0, 8192.0, 1.0, 4.0)
