@@ -7,15 +7,16 @@
 //
 // i-exp needs the row's maximum before the first exponential (its shifts do not commute with a later maximum), so the
 // scores are computed twice: pass A takes the maximum of all score tiles, pass B recomputes them, weights them and
-// multiplies with V.  The second Q K^T costs the tensor pipe 64 of the 1400 clocks that the exponentials of a tile take;
-// in exchange O is never rescaled and accumulates in tensor memory as exact integers.
+// multiplies with V.  The tensor pipe is idle for most of a tile's exponentials either way (14 % busy with both products and
+// the second Q K^T); in exchange O is never rescaled and accumulates in tensor memory as exact integers.
 //
 // A CTA takes 128 consecutive ROWS of the packed tensor, whatever sequences they belong to, and one head: keys run from
 // the first row's first visible key to the last row, each row with bounds of its own.  So short sequences share tiles,
 // and the grid follows from the row count alone.  Four warps, a thread per query row (= TMEM lane), and one that issues
-// copies and products; four CTAs per SM (128
-// columns of tensor memory each: 64 scores, 64 context values; pass A, which has no context yet, takes 128 scores at a
-// time) hide each other's waits.
+// copies and products; four CTAs per SM (128 columns of tensor memory each: 64 scores, 64 context values; pass A, which has
+// no context yet, uses both halves for scores in turn) hide each other's waits.
+// Bound by the multiply-add pipe through the exponentials.  8192 tokens, 16 heads, window 2048 + 4: 138 us, 2.1e12 scores a
+// second; with one barrier of the whole CTA per step, and no warp for copies and products, it was 200.
 #include <cuda.h>
 
 #include <algorithm>
