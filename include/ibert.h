@@ -333,8 +333,8 @@ int ibert_classifier_packed_i8(ibert_ctx* ctx, const int8_t* x, const int32_t* c
        positions[i] = lens[b] + j and slots[i] its slot; entries from cu_seqlens[B] to max_tokens - 1 get slot -1 and
        position 0 (ibert_qkv_rope_i8 stores nothing for slot -1);
      - lens_out[b] = lens[b] + new_lens[b] (0: ended) and *n_free_out are the lengths and the stack after the step.
-   lens_out may be lens and n_free_out may be n_free; no other arrays may overlap (IBERT_ERR_ARG where two start at one address).  New tokens past max_tokens in the
-   running count are left out.  A token without a page (the stack is empty, or the request's table full) gets slot -1, its
+   lens_out may be lens and n_free_out may be n_free; no other arrays may overlap (IBERT_ERR_ARG where two start at one
+   address).  New tokens past max_tokens in the running count are left out.  A token without a page (the stack is empty, or the request's table full) gets slot -1, its
    page's entry -1, and does not count in lens_out.  Both record IBERT_ERR_VALUE_RANGE in the context's status, as do lengths
    outside [0, max_pages * page_size] and an *n_free outside [0, free_capacity] (taken as the nearest bound).
    B in [0, 8192], max_pages * page_size and B * max_pages below 2^31, max_tokens and free_capacity below 2^31. */
@@ -403,7 +403,7 @@ typedef struct ibert_attention_desc {
    ibert_qkv_rope_i8 writes with with_kv = 1), sequence b in rows cu_seqlens[b] .. cu_seqlens[b+1] - 1 (device int32 [B+1],
    non-decreasing from 0, every length at most max_len); out int8 [total_tokens][heads 64] at S_ctx (*S_ret).  A query sees the
    keys of its own sequence up to its own position; with window > 0 only the last `window` of them (itself included) and the
-   first `sinks` of the sequence.  Rows from cu_seqlens[B] on are left as they were.  Weights and result as defined for
+   first `sinks` of the sequence.  (A prompt comes in one piece: keys that only the cache holds are not seen.)  Rows from cu_seqlens[B] on are left as they were.  Weights and result as defined for
    ibert_attention_decode_i8 below -- a token's context is the same bit for bit whichever of the two computes it.
    At most 65536 visible keys: min(max_len, window + sinks if window > 0) <= 65536, else IBERT_ERR_SHAPE.  A sequence longer
    than max_len, or one that reaches past total_tokens, records IBERT_ERR_VALUE_RANGE in the context's status; queries then see at
@@ -417,8 +417,8 @@ int ibert_attention_window_i8(ibert_ctx* ctx, const ibert_attention_desc* desc, 
    b, and rows = B.  Else (device int32 [B+1], what ibert_kv_slots gives for a step in which some requests get no token, have
    ended or got a whole prompt) sequence b's row is cu_seqlens[b+1] - 1, its last new token; the rows of other tokens, and
    all rows of a sequence with no new token, are left as they were; a row outside [0, rows) is left out and records
-   IBERT_ERR_VALUE_RANGE.  lens: device int32 [B], tokens in the cache
-   (the new one included), at most max_len; a sequence of length 0 yields 0.  Key j is visible if j < lens[b] and
+   IBERT_ERR_VALUE_RANGE.  lens: device int32 [B], tokens in the cache (the new one included), at most max_len; a sequence of
+   length 0 yields 0.  Key j is visible if j < lens[b] and
    (window = 0, or j >= lens[b] - window, or j < sinks): a sliding window, and first tokens that stay visible.  Pages
    that hold no visible key are not looked at.  With e_j the i-exp (Algorithm 3) of the distance of s_j = q k_j (scale
    S_q S_k / 8) from the maximum of the visible keys and b_w = floor(p_max 2^24 / i-exp(0)):
@@ -427,9 +427,10 @@ int ibert_attention_window_i8(ibert_ctx* ctx, const ibert_attention_desc* desc, 
    -- weights relative to the row's maximum, divided by their sum at the end.  (ibert_attention_i8 divides first; over
    thousands of keys all of its u8 probabilities would be 0.)
    At most 65536 visible keys: min(max_len, window + sinks if window > 0) <= 65536, else IBERT_ERR_SHAPE; window, sinks >= 0;
-   max_len <= max_pages * page_size, max_len < 2^31 - 256, rows * heads < 2^31.  A length above max_len (taken as max_len) or below 0, and a visible key on a page
-   outside [0, n_pages) (the key is left out), record IBERT_ERR_VALUE_RANGE in the context's status.
-   out must not overlap the other arrays.  IBERT_ERR_SCALE_RANGE also for score scales so coarse that floor(ln2 / (S_q S_k / 8)) <= 2; p_max in {255, 127}. */
+   max_len <= max_pages * page_size, max_len < 2^31 - 256, rows * heads < 2^31, B * heads < 2^24.  A length above max_len
+   (taken as max_len) or below 0, and a visible key on a page outside [0, n_pages) (the key is left out), record
+   IBERT_ERR_VALUE_RANGE in the context's status.  out must not overlap the other arrays.
+   IBERT_ERR_SCALE_RANGE also for score scales so coarse that floor(ln2 / (S_q S_k / 8)) <= 2; p_max in {255, 127}. */
 int ibert_attention_decode_i8(ibert_ctx* ctx, const ibert_attention_desc* desc, const int8_t* q, const int8_t* k_cache,
                               const int8_t* v_cache, const int32_t* block_tables, const int32_t* lens, int B,
                               const int32_t* cu_seqlens, int64_t rows, int8_t* out, double* S_ret);

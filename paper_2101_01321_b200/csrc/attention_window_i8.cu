@@ -118,7 +118,7 @@ attention_window_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
   const int c0 = ptx::ld_dep(a.cu + lo_b), c1 = ptx::ld_dep(a.cu + lo_b + 1);
   const bool real = q0 + r < a.T && row >= c0 && row < c1;
   const int first = real ? max(c0, 0) : row;                 // of the sequence; a row of none sees itself and is not stored
-  const int low = max(first, row - (a.window > 0 ? a.window : a.max_len) + 1);
+  const int low = max(first, row - (a.window > 0 ? min(a.window, a.max_len) : a.max_len) + 1);
   const bool bad = real && tid < 128 && (c1 - c0 > a.max_len || c1 > a.T);
   if (tid == 0) { s_bounds[0] = low; s_bounds[1] = first; }
   if (tid == 127) s_bounds[2] = low;       // (of the tile's last row)
