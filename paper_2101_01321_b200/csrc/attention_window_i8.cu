@@ -377,7 +377,7 @@ int launch_attention_window(ibert_ctx* ctx, const int8_t* qkv, const int32_t* cu
   const int64_t grid = (int64_t)a.tiles * heads;
   if (grid > INT32_MAX) return IBERT_ERR_SHAPE;
   const int mode = k.short_k ? 3 : (!iexp_takes_folded(k.e) ? 2 : (k.e.s_in == 0 ? 0 : 1));
-  const bool split = grid <= 4 * (int64_t)ctx->num_sms;
+  const bool split = grid <= 2 * (int64_t)ctx->num_sms;      // (as many as are resident so; 512 CTAs of equal length 86 us, unsplit 74)
   decltype(&attention_window_kernel<0, 1>) const kernels[2][4] = {
       {attention_window_kernel<0, 1>, attention_window_kernel<1, 1>, attention_window_kernel<2, 1>, attention_window_kernel<3, 1>},
       {attention_window_kernel<0, 2>, attention_window_kernel<1, 2>, attention_window_kernel<2, 2>, attention_window_kernel<3, 2>}};
