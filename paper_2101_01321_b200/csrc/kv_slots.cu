@@ -15,7 +15,6 @@
 namespace ibert {
 namespace {
 
-
 constexpr int kSlotThreads = 1024;
 
 struct SlotArgs {
@@ -207,9 +206,15 @@ int launch_kv_slots(ibert_ctx* ctx, const int32_t* lens, const int32_t* new_lens
   SlotArgs a{lens, new_lens, tables, stack, n_free, B, log_page, max_pages, in_place, capacity, max_tokens,
              lens_out, n_free_out, cu, slots, positions, ctx->d_status};
   const size_t smem = (4 * (size_t)B + 3) * sizeof(int32_t);
-  if (smem > 40 * 1024 && cudaFuncSetAttribute(kv_slots_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) {
-    cudaGetLastError();
-    return IBERT_ERR_CUDA;
+  static bool set[kMaxDevices] = {false};
+  bool& done = set[ctx->device % kMaxDevices];
+  if (!done) {                             // (for the largest batch, not this one: other threads' launches have the same limit)
+    if (cudaFuncSetAttribute(kv_slots_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                             (4 * kMaxRequests + 3) * (int)sizeof(int32_t)) != cudaSuccess) {
+      cudaGetLastError();
+      return IBERT_ERR_CUDA;
+    }
+    done = true;
   }
   return launch_pdl(kv_slots_kernel, dim3(ctas), dim3(kSlotThreads), smem, ctx->stream, in_place ? ctas : 1, a);
 }

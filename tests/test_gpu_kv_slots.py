@@ -1,9 +1,12 @@
 """Block tables and slot maps on the GPU against the plain form: whole steps, in place, and everything that runs out."""
+import threading
+
 import numpy as np
 import pytest
 import torch
 
 import generation_reference as ref
+from paper_2101_01321_b200 import binding
 from gpu_util import assert_same, ctx, dev, host
 
 pytestmark = pytest.mark.gpu
@@ -136,3 +139,37 @@ def test_many_steps_of_one_pool():
         held = np.concatenate([t[b, :-(-n[b] // P)] for b in range(B)])
         held = held[held >= 0]
         assert np.unique(np.concatenate([held, s])).size == held.size + s.size <= pool
+
+
+def test_two_host_threads_with_batches_of_different_sizes():
+    """Every launch finds the shared memory that it asks for, whatever another thread launches in between.  (The step is not in
+    place, so it gives the same again and again.)"""
+    rng = np.random.default_rng(12)
+    work, errors = [], []
+    for B in (8192, 3000):
+        st = _state(rng, B, 16, 6, 90, ONE)
+        d, sizes = [dev(a) for a in st], dict(lens_out=B, n_free_out=1, cu_seqlens=B + 1, slots=B, positions=B)
+        out = {name: torch.empty(n, dtype=torch.int32, device="cuda") for name, n in sizes.items()}
+        work.append((binding.Context(0, stream=torch.cuda.Stream()), d, out, ref.kv_slots(*st[:4], st[4][0], 16, B)))
+    torch.cuda.synchronize()
+    start = threading.Barrier(len(work))
+
+    def run(c, d, out):
+        try:
+            start.wait(30)
+            for _ in range(1500):
+                c.ibert_kv_slots(*d, 16, **out)
+        except Exception as e:  # noqa: BLE001 -- for the test's own thread
+            errors.append(e)
+
+    threads = [threading.Thread(target=run, args=w[:3]) for w in work]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert not errors
+    for c, d, out, want in work:
+        c.check()
+        for g, w in zip([*out.values(), d[2], d[3]], [want[0], np.array([want[1]]), *want[2:7]]):
+            assert_same(host(g), w)
