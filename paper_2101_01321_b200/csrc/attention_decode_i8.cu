@@ -19,7 +19,7 @@
 // the operand of both K steps as they come (any order of the 64 dimensions will do if Q has the same); the values are
 // transposed on their way out of shared memory (ldmatrix of bytes), four keys to a register.
 // Measured: 64 sequences of up to 2048 keys, 16 heads of their own 28 us (5.3 TB/s, 0.82 of the copy rate); 16 of up to 32768,
-// 32 heads over 4: 33 us (3.6 TB/s), bound by issue; one of 1000: 5.0 us, a chain of five dependent loads and two barriers.
+// 32 heads over 4: 33 us (3.6 TB/s; 40 when nothing of it is in L2), bound by issue; one of 1000: 5.0 us, a chain of five dependent loads and two barriers.
 #include <algorithm>
 
 #include "device_utils.cuh"
