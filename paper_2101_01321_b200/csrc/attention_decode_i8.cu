@@ -85,6 +85,9 @@ attention_decode_kernel(const __grid_constant__ DecodeArgs a) {
   const uint32_t rank = ptx::cluster_ctarank();
   int cl;
   asm("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(cl));
+  // (The shared memory of a CTA may be written by another one only once it runs: every CTA says so here and waits for the others
+  // before its first store to them, behind its keys.)
+  if (cl > 1) ptx::cluster_arrive();
   const int item = (int)blockIdx.x / cl;
   const int piece = item % a.tiles_of_group, pair = item / a.tiles_of_group;
   const int kvh = pair % a.kv_heads;
@@ -208,6 +211,7 @@ attention_decode_kernel(const __grid_constant__ DecodeArgs a) {
   mx = max(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
   if (t == 0) s_warp_max[warp][g] = mx;
   __syncthreads();
+  if (cl > 1) ptx::cluster_wait();       // (every CTA of the cluster runs)
   for (int i = tid; i < cl * kMaxGroup; i += kThreads) {      // this CTA's maxima into every CTA of the cluster
     const int h = i & (kMaxGroup - 1), to = i / kMaxGroup;
     int32_t m = s_warp_max[0][h];
