@@ -407,7 +407,7 @@ typedef struct ibert_attention_desc {
    ibert_attention_decode_i8 below -- a token's context is the same bit for bit whichever of the two computes it.
    At most 65536 visible keys: min(max_len, window + sinks if window > 0) <= 65536, else IBERT_ERR_SHAPE.  A sequence longer
    than max_len, or one that reaches past total_tokens, records IBERT_ERR_VALUE_RANGE in the context's status; queries then see at
-   most their last max_len keys and the sinks.  out must not overlap qkv.
+   most their last max_len keys and the sinks, of these as many as 65536 keys in all leave room for.  out must not overlap qkv.
    total_tokens < 2^31 - 256; scale and p_max errors as below. */
 int ibert_attention_window_i8(ibert_ctx* ctx, const ibert_attention_desc* desc, const int8_t* qkv, const int32_t* cu_seqlens,
                               int B, int64_t total_tokens, int8_t* out, double* S_ret);

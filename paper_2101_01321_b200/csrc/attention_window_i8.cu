@@ -372,7 +372,10 @@ int launch_attention_window(ibert_ctx* ctx, const int8_t* qkv, const int32_t* cu
   if (int rc = encode_tensor_map(&mkv, qkv, 2, dims, str, box_kv, 64)) return rc;
   WindowArgs a{};
   a.cu = cu; a.out = out; a.status = ctx->d_status;
-  a.T = (int32_t)T; a.B = B; a.max_len = max_len; a.heads = heads; a.kv_heads = kv_heads; a.window = window; a.sinks = sinks;
+  a.T = (int32_t)T; a.B = B; a.max_len = max_len; a.heads = heads; a.kv_heads = kv_heads; a.window = window;
+  // (sequences of up to max_len lose nothing: where this cuts, they have at most 65536 keys and all of them are seen; longer
+  // ones, which are reported, keep their sums in 32 bits)
+  a.sinks = std::min(sinks, kMaxVisible - std::min({window, max_len, kMaxVisible}));
   a.tiles = (int32_t)((T + 127) / 128); a.int_min = INT32_MIN; a.k = k;
   const int64_t grid = (int64_t)a.tiles * heads;
   if (grid > INT32_MAX) return IBERT_ERR_SHAPE;
