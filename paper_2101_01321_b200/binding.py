@@ -7,6 +7,7 @@ from __future__ import annotations
 
 import ctypes as C
 import struct
+import threading
 from pathlib import Path
 
 import numpy as np
@@ -203,6 +204,15 @@ def ibert_rope_rows(inv_freq, n: int, factor: float = 1.0, pos0: int = 0) -> np.
     return rows
 
 
+class _Gammas(threading.local):
+    """The factors of an ``ibert_qkv_rope_i8`` call, at addresses that are looked up once.  Each thread has its own: the library
+    reads them during the call, while another thread may make one."""
+
+    def __init__(self):
+        self.values = np.zeros((2, 64))
+        self.ptrs = [self.values[i].ctypes.data for i in range(2)]
+
+
 class Context:
     """``ibert_ctx``: a device and the stream every call is enqueued on."""
 
@@ -213,8 +223,7 @@ class Context:
         sp = None if stream is None else stream.cuda_stream
         _chk(lib().ibert_create(C.byref(h), device, sp), "ibert_create")
         self.h = h
-        self._gammas = np.zeros((2, 64))     # ibert_qkv_rope_i8's, at addresses that are looked up once
-        self._gamma_ptrs = [self._gammas[i].ctypes.data for i in range(2)]
+        self._gammas = _Gammas()
 
     def close(self):
         if self.h:
@@ -537,12 +546,13 @@ class Context:
         dtype = qkv.dtype
         assert qkv.numel() == T * n and (dtype is torch.int8 or dtype is torch.int16)
         gq = gk = 0
+        g = self._gammas
         if gamma_q is not None:              # (read during the call)
             assert len(gamma_q) == 64
-            self._gammas[0], gq = gamma_q, self._gamma_ptrs[0]
+            g.values[0], gq = gamma_q, g.ptrs[0]
         if gamma_k is not None:
             assert len(gamma_k) == 64
-            self._gammas[1], gk = gamma_k, self._gamma_ptrs[1]
+            g.values[1], gk = gamma_k, g.ptrs[1]
         max_pos = rot_dim = n_pages = page_size = 0
         if rope is not None:
             max_pos, rot_dim = rope.shape
