@@ -381,7 +381,7 @@ typedef struct ibert_rope_desc {
    qkv: device [T][(heads + 2 kv_heads) 64], columns Q | K | V.  positions: device int32 [T] (may be NULL if rot_dim is 0).
    out: device int8, with_kv 1: [T][(heads + 2 kv_heads) 64], the layout of qkv; with_kv 0: [T][heads 64], Q alone.
    k_cache, v_cache, slots (device int32 [T]): K and V also go to their slots of the cache; slot -1 stores nothing; all three
-   NULL: no cache.  Two tokens must not have the same slot.  out and the cache must not overlap qkv or each other.
+   NULL: no cache (slots may be NULL for T = 0).  Two tokens must not have the same slot.  out and the cache must not overlap qkv or each other.
    S_ret (host, may be NULL) receives S_q, S_k, S_v.
    A position outside [0, max_pos) (taken as 0) or a slot outside [-1, n_pages * page_size) (taken as -1) records
    IBERT_ERR_VALUE_RANGE in the context's status.  n_pages * page_size below 2^31; table entries with c^2 + s^2 <= 2^30. */

@@ -1167,7 +1167,7 @@ int ibert_qkv_rope_i8(ibert_ctx* ctx, const ibert_rope_desc* d, const void* qkv,
       d->rot_dim < 0 || d->rot_dim > 64 || d->rot_dim % 8 != 0 || T >= (int64_t(1) << 31))
     return IBERT_ERR_SHAPE;
   if (!d->gamma_q != !d->gamma_k) return IBERT_ERR_ARG;
-  if (!k_cache != !v_cache || !k_cache != !slots) return IBERT_ERR_ARG;
+  if (!k_cache != !v_cache || (slots ? !k_cache : k_cache && T > 0)) return IBERT_ERR_ARG;
   RopeArgs a{};
   if (k_cache) {
     a.log_page = log2_page(d->page_size);
