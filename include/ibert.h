@@ -354,7 +354,8 @@ int ibert_rope_frequencies(int rot_dim, double base, double stretch, double trai
                            double high_turns, double* inv_freq);
 /* Host, pure.  Rows pos0 .. pos0 + n - 1 of the rotation table that ibert_qkv_rope_i8 reads from device memory:
    rows[p][2i], rows[p][2i+1] = round-half-up(2^14 factor cos a), round-half-up(2^14 factor sin a) with the angle
-   a = (pos0 + p) inv_freq[i] in double precision.  factor in (0, 1.99] (an attention temperature; usually 1). */
+   a = (pos0 + p) inv_freq[i] in double precision.  factor in (0, 1.99] (an attention temperature; usually 1).
+   IBERT_ERR_ARG also for an angle that is not finite and for positions past 2^63 - 1. */
 int ibert_rope_rows(const double* inv_freq, int rot_dim, int64_t pos0, int64_t n, double factor, int16_t* rows);
 
 typedef struct ibert_rope_desc {

@@ -1147,8 +1147,10 @@ int ibert_rope_rows(const double* inv_freq, int rot_dim, int64_t pos0, int64_t n
   if (rot_dim < 8 || rot_dim > 64 || rot_dim % 8 != 0) return IBERT_ERR_SHAPE;
   if (!inv_freq || n < 0 || pos0 < 0 || (n > 0 && !rows)) return IBERT_ERR_ARG;
   if (!std::isfinite(factor) || !(factor > 0.0) || factor > 1.99) return IBERT_ERR_ARG;
+  if (n > 0 && pos0 > INT64_MAX - (n - 1)) return IBERT_ERR_ARG;
+  const double last = n > 0 ? (double)(pos0 + (n - 1)) : 0.0;     // (the largest angle of every frequency is the last one's)
   for (int i = 0; i < rot_dim / 2; ++i)
-    if (!std::isfinite(inv_freq[i])) return IBERT_ERR_ARG;
+    if (!std::isfinite(inv_freq[i]) || !std::isfinite(last * inv_freq[i])) return IBERT_ERR_ARG;
   for (int64_t p = 0; p < n; ++p)
     for (int i = 0; i < rot_dim / 2; ++i) {
       const double angle = (double)(pos0 + p) * inv_freq[i];
