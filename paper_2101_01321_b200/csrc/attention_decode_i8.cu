@@ -14,12 +14,14 @@
 // is written.
 //
 // The products run on mma.sync m16n8k32 (s8 x s8, s8 x u8): up to eight query heads of a group, and the kernel is bound by
-// the 128 bytes per key and the instructions around them, not by the tensor pipe.  S^T = Q K^T leaves a lane with one head
+// the 128 bytes per key and the latency of getting them, not by the tensor pipe (15 % busy).  S^T = Q K^T leaves a lane with one head
 // and the very keys whose weights it needs as the B operand of O^T = V^T w; the 16 bytes of a key that a lane copies are
 // the operand of both K steps as they come (any order of the 64 dimensions will do if Q has the same); the values are
 // transposed on their way out of shared memory (ldmatrix of bytes), four keys to a register.
-// Measured: 64 sequences of up to 2048 keys, 16 heads of their own 28 us (5.3 TB/s, 0.82 of the copy rate); 16 of up to 32768,
-// 32 heads over 4: 33 us (3.6 TB/s; 40 when nothing of it is in L2), bound by issue; one of 1000: 5.0 us, a chain of five dependent loads and two barriers.
+// Measured, with what one pass leaves in L2 for the next / with nothing there: 64 sequences of up to 2048 keys, 16 heads of their own 28 / 29 us
+// (5.2 TB/s, 0.79 of the copy rate); 16 of up to 32768, 32 heads over 4: 33 / 39 us (3.0 TB/s), where neither issue (47 % of the slots) nor
+// HBM (39 %) is full: warps wait for loads and barriers, and the CTAs of the long sequences, as many as the short ones have, run on alone
+// (SMs are active for 69 % of the time); one of 1000: 5.0 us, a chain of five dependent loads and the barriers of its cluster.
 #include <algorithm>
 
 #include "device_utils.cuh"
@@ -31,7 +33,7 @@ namespace {
 constexpr int kTile = 32;                // keys a warp takes at a time
 constexpr int kTileBytes = kTile * kHeadDim;
 constexpr int kMaxGroup = 8;             // query heads per CTA
-constexpr int kMaxCluster = 8;           // (larger ones find no place on the GPU for long: 16 x 32768 x 32 heads 55 us at 16, 38 at 8)
+constexpr int kMaxCluster = 8;           // (larger ones find no place on the GPU for long: 16 x 32768 x 32 heads 55 us at 16 where 8 took 38, now 33)
 constexpr int kDecMaxSmem = 160 * 1024;
 
 struct DecodeArgs {
@@ -68,8 +70,10 @@ __device__ __forceinline__ void mma_s8u8(int32_t (&c)[4], uint32_t a0, uint32_t 
 // W warps with STAGES tiles of each in flight.  KEEP: the scores stay in shared memory from the maximum to the weights, and the
 // exponentials of a head are spread over all threads; else the keys are read a second time (out of L2) and every lane computes
 // the weights that it needs itself.  For one or two heads the eight weights per lane and tile would be those of an eighth or a
-// quarter of the lanes (64 x 2048, 16 heads of their own: 28 us kept); for more, the scores' 4 bytes per head and key take the
-// shared memory that the loads in flight need (16 x 32768, 8 heads each: 69 us kept, in clusters of 16, 38 read again in 8).
+// quarter of the lanes; for more, the scores' 4 bytes per head and key take the shared memory that the loads in flight need.  Kept / read
+// again, us: 8 heads, 64 x 2048 26 / 14, 128 with a window of 1024 33 / 17; 3 heads, 16 x 32768 41 / 33, 4 heads 44 / 33, one of 1000
+// 6.6 / 5.5.  Where 3 or 4 heads see few keys and sequences are many, the rule by heads alone loses some: 64 x 2048 12 / 14 and 13 / 14,
+// 128 with a window of 1024 13 / 16 and 14 / 16.
 template <int W, int STAGES, bool KEEP>
 __global__ void __launch_bounds__(32 * W, KEEP ? 5 : 4)
 attention_decode_kernel(const __grid_constant__ DecodeArgs a) {
@@ -350,7 +354,9 @@ int launch_attention_decode(ibert_ctx* ctx, const int8_t* q, const int8_t* k_cac
   a.log_page = log_page; a.max_pages = max_pages; a.n_pages = n_pages; a.max_len = max_len; a.window = window; a.sinks = sinks;
   a.k = k;
   const int64_t items = (int64_t)B * kv_heads * a.tiles_of_group;
-  // tiles of 32 keys that a sequence can have: one more where the window starts inside a tile, and the sinks' own
+  // Tiles of 32 keys that a sequence can have: one more where the window starts inside a tile, and the sinks' own.  The lengths are on the
+  // device, so the plan is max_len's, and kept scores take shared memory for that many keys: 64 sequences of up to 2048, 16 heads of
+  // their own, 29 us with a max_len of 2048, 31 with 8192, 56 with 32768 and 91 with 65536 (read again: the same with each).
   int64_t tiles = ((int64_t)max_len + kTile - 1) / kTile;
   if (window > 0) tiles = std::min<int64_t>(tiles, ((int64_t)window + kTile - 1) / kTile + 1 + ((int64_t)sinks + kTile - 1) / kTile);
   const bool keep = a.group <= 2;

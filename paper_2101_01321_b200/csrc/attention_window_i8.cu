@@ -7,7 +7,7 @@
 //
 // i-exp needs the row's maximum before the first exponential (its shifts do not commute with a later maximum), so the
 // scores are computed twice: pass A takes the maximum of all score tiles, pass B recomputes them, weights them and
-// multiplies with V.  The tensor pipe is idle for most of a tile's exponentials either way (14 % busy with both products and
+// multiplies with V.  The tensor pipe is idle for most of a tile's exponentials either way (16 % busy with both products and
 // the second Q K^T); in exchange O is never rescaled and accumulates in tensor memory as exact integers.
 //
 // A CTA takes 128 consecutive ROWS of the packed tensor, whatever sequences they belong to, and one head: keys run from
@@ -15,8 +15,10 @@
 // and the grid follows from the row count alone.  Four warps, a thread per query row (= TMEM lane), and one that issues
 // copies and products; four CTAs per SM (128 columns of tensor memory each: 64 scores, 64 context values; pass A, which has
 // no context yet, uses both halves for scores in turn) hide each other's waits.
-// Bound by the multiply-add pipe through the exponentials.  8192 tokens, 16 heads, window 2048 + 4: 138 us, 2.1e12 scores a
-// second; with one barrier of the whole CTA per step, and no warp for copies and products, it was 200.
+// Bound by the instructions of the exponentials, 11.5 per 32 scores with maxima and masks.  8192 tokens, 16 heads, window 2048 + 4: 138 us,
+// 2.1e12 scores a second; issue slots 70 % and the ALU pipe 66 % busy (88 and 83 us of it, multiply-adds 65), the rest are waits, instruction
+// fetch and SMs that are done early.  With one barrier of the whole CTA per step, and no warp for copies and products, it was 200.
+// Of prompts of unequal length the longest rows' CTAs decide: 5 of up to 1531, 560 CTAs in one wave, 50 us, SMs active for 64 % of it.
 #include <cuda.h>
 
 #include <algorithm>
@@ -53,8 +55,8 @@ __device__ __forceinline__ uint64_t bits_between(int a, int b) {
 __device__ __forceinline__ uint32_t byte_mask(uint32_t m) { return ((m & 15u) * 0x00204081u & 0x01010101u) * 255u; }
 
 // MODE: how i-exp is evaluated; 0: folded without a pre-shift, 1: folded with one, 2: the wide form, 3: with the quotient in 32
-// bits.  The exponentials bind the kernel through the multiply-add pipe, two clocks per warp and instruction there, four for the
-// upper word of a product: 10.5 clocks per score in the folded form, 8.5 (and 7.5 on the ALU pipe) with the short quotient.
+// bits.  On the multiply-add pipe an instruction takes two clocks per warp, four for the upper word of a product: 10.5 clocks per
+// score's exponential in the folded form, 8.5 (and 7.5 on the ALU pipe) with the short quotient.
 // SPLIT: threads per row, each with half of a tile's columns: while the CTAs are few, their rows' exponentials are the longest
 // part of every step (4 prompts of up to 97 tokens, 12 heads, 36 CTAs: 8.6 us by one thread, 8.0 by two; 1 x 2048 x 16 heads, 256 CTAs: 40 and 37)
 template <int MODE, int SPLIT>
@@ -380,7 +382,10 @@ int launch_attention_window(ibert_ctx* ctx, const int8_t* qkv, const int32_t* cu
   const int64_t grid = (int64_t)a.tiles * heads;
   if (grid > INT32_MAX) return IBERT_ERR_SHAPE;
   const int mode = k.short_k ? 3 : (!iexp_takes_folded(k.e) ? 2 : (k.e.s_in == 0 ? 0 : 1));
-  const bool split = grid <= 2 * (int64_t)ctx->num_sms;      // (as many as are resident so; 512 CTAs of equal length 86 us, unsplit 74)
+  // As many CTAs as are resident so.  Split / not, us, for some 500 CTAs: rows of equal work 86 / 74 (8192 tokens with a window), 22 / 18 (60
+  // prompts of up to 128; 100 of up to 80).  Where the work is unequal they would gain, 45 / 49 (5 prompts of up to 1531), 84 / 94 (one of
+  // 4096), 59 / 66 (3 of up to 2000), but the host does not know the lengths.
+  const bool split = grid <= 2 * (int64_t)ctx->num_sms;
   decltype(&attention_window_kernel<0, 1>) const kernels[2][4] = {
       {attention_window_kernel<0, 1>, attention_window_kernel<1, 1>, attention_window_kernel<2, 1>, attention_window_kernel<3, 1>},
       {attention_window_kernel<0, 2>, attention_window_kernel<1, 2>, attention_window_kernel<2, 2>, attention_window_kernel<3, 2>}};

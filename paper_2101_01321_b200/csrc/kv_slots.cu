@@ -199,8 +199,8 @@ kv_slots_kernel(const SlotArgs a) {
 int launch_kv_slots(ibert_ctx* ctx, const int32_t* lens, const int32_t* new_lens, int32_t* tables, int32_t* stack,
                     const int32_t* n_free, int B, int log_page, int max_pages, int64_t capacity, int64_t max_tokens,
                     int32_t* lens_out, int32_t* n_free_out, int32_t* cu, int32_t* slots, int32_t* positions) {
-  // Written in place, the lengths must have been read by all CTAs before: one cluster, eight CTAs.  Else as many as there are
-  // tokens for, four at least (256 requests and a token for each, some pages given back: one CTA 7.2 us, four 5.2; 131,000 tokens 20.5 by eight, 6.9).
+  // Written in place, the lengths must have been read by all CTAs before: one cluster, eight CTAs (256 requests and a token for each, some
+  // pages given back 5.4 us, 131,000 tokens 25).  Else as many as there are tokens for, four at least (5.1, by one CTA 7.2; 131,000 tokens 6.8).
   const bool in_place = lens_out == lens || n_free_out == n_free;
   const int ctas = in_place ? 8 : (int)std::min<int64_t>(ctx->num_sms, std::max<int64_t>(4, (max_tokens + B) / kSlotThreads + 1));
   SlotArgs a{lens, new_lens, tables, stack, n_free, B, log_page, max_pages, in_place, capacity, max_tokens,
