@@ -188,7 +188,7 @@ int make_head_norm(const double* gamma, double S_out, int16_t* b, int32_t* g) {
     top = std::max(top, std::fabs(gamma[i] * unit));
   }
   int e = top > 0.0 ? (int)std::min(16.0, std::floor(std::log2(32767.0 / top))) : 16;
-  while (std::floor(std::ldexp(top, e) + 0.5) > 32767.0) --e;     // (a logarithm rounded up)
+  while (std::ldexp(top, e) > 32767.0) --e;        // (a logarithm rounded up)
   if (e < -8) return IBERT_ERR_SCALE_RANGE;
   for (int i = 0; i < 64; ++i) {
     const double m = std::floor(std::ldexp(std::fabs(gamma[i] * unit), e) + 0.5);
